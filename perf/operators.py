@@ -285,10 +285,10 @@ def _exact_values(q, scales, weight):
     return v
 
 
-def _exact_quantized(y, block_rows):
-    """e4m3 elements and scales of y as 64-bit values."""
+def _exact_scaled(y, block_rows):
+    """y over the scales of its blocks, before any rounding, and the scales."""
     rows, cols = y.shape
-    q = torch.empty_like(y)
+    t = torch.empty_like(y)
     scales = torch.ones(-(-rows // block_rows), _pitch(cols), dtype=torch.float64, device=y.device)
     for b in range(-(-cols // 128)):
         part = y[:, 128 * b:128 * b + 128]
@@ -300,11 +300,16 @@ def _exact_quantized(y, block_rows):
         scale = torch.where(448.0 * low >= largest, low, 2.0 * low)
         scale = torch.where(largest == 0.0, torch.ones_like(scale), scale.clamp(2.0 ** -127, 2.0 ** 127))
         scales[:, b] = scale
-        t = part / scale[torch.arange(rows, device=y.device) // block_rows][:, None]
-        _, top = torch.frexp(t)
-        step = torch.exp2((top - 1).clamp(min=-6).double() - 3.0)    # three fraction bits; subnormals below 2^-6
-        q[:, 128 * b:128 * b + 128] = torch.round(t / step) * step
-    return q, scales
+        t[:, 128 * b:128 * b + 128] = part / scale[torch.arange(rows, device=y.device) // block_rows][:, None]
+    return t, scales
+
+
+def _exact_stored(y):
+    """The values that y's rows stand for once they are held in 8 bits: what a next operator reads."""
+    t, scales = _exact_scaled(y, 1)
+    _, top = torch.frexp(t)
+    step = torch.exp2((top - 1).clamp(min=-6).double() - 3.0)    # three fraction bits; subnormals below 2^-6
+    return torch.round(t / step) * step * scales.repeat_interleave(128, dim=1)[:, :t.shape[1]]
 
 
 def _exact_rms(s):
@@ -324,22 +329,21 @@ def _exact_linear(a, w, bias, gelu):
 
 
 def exact(case, seed):
+    # (8-bit results, like those in bf16, are given as they are before they are rounded for storage)
     s, op = prepare(case, seed), case["op"]
     if op == "rms":
         y, h = _exact_rms(s)
-        q, scales = _exact_quantized(y, 1)
+        q, scales = _exact_scaled(y, 1)
         return {"q": q, "scales": scales, "sum": h if case["sum"] else None}
     if op == "quantize":
-        q, scales = _exact_quantized(s["x"].double(), case["block_rows"])
+        q, scales = _exact_scaled(s["x"].double(), case["block_rows"])
         return {"q": q, "scales": scales}
     if op == "linear":
         v = _exact_linear(_exact_values(s["a"], s["a_scales"], False), _exact_values(s["w"], s["w_scales"], True), s["bias"], case["gelu"])
         if case["quantized"]:
-            q, scales = _exact_quantized(v, 1)
+            q, scales = _exact_scaled(v, 1)
             return {"q": q, "scales": scales}
         return {"c": v}
-    q, scales = _exact_quantized(_exact_rms(s)[0], 1)
     w1, w2 = _exact_values(s["w1"], s["w1_scales"], True), _exact_values(s["w2"], s["w2_scales"], True)
-    factor = scales.repeat_interleave(128, dim=1)[:, :q.shape[1]]
-    mid, mid_scales = _exact_quantized(_exact_linear(q * factor, w1, s["bias1"], True), 1)
-    return {"c": _exact_linear(mid * mid_scales.repeat_interleave(128, dim=1)[:, :mid.shape[1]], w2, s["bias2"], False)}
+    mid = _exact_stored(_exact_linear(_exact_stored(_exact_rms(s)[0]), w1, s["bias1"], True))
+    return {"c": _exact_linear(mid, w2, s["bias2"], False)}
