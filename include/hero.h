@@ -357,6 +357,48 @@ int hero_second_diff_stats(const void* f_prev, const void* f_cur, const void* f_
  * (1 - (v - min) / (max - min); all equal -> 1). */
 int hero_stability_scores(const double* variances, int32_t n_layers, double* scores);
 
+/* ---- 8-bit linear layers ------------------------------------------------------------
+ * Rows and weights in 8 bits: e4m3 elements (OCP: largest value 448, no infinities, 0x7F / 0xFF is NaN), row-major and
+ * contiguous, and a scale for every block of 128 consecutive columns of a row, or of 128 x 128 elements of a weight (the
+ * last blocks of a row or column of blocks may be shorter).  A scale is a power of two in one byte (E8M0): an element
+ * stands for its value * 2^(byte - 127); byte 255 is NaN, and so is everything in its block.  The scales of a row (of a
+ * weight: of 128 rows) are HERO_FP8_SCALE_PITCH(columns) bytes apart, a whole number of 32-bit words; the bytes that fill the
+ * last word are written as 127 and never used.  Column counts are multiples of 16.
+ * A block is put into 8 bits with the least scale that takes its largest finite magnitude to 448 or below (byte 127 if that is
+ * 0; never below byte 0), every element rounded to nearest, ties to even; NaN and infinities become NaN elements and do not
+ * count for the scale. */
+#define HERO_FP8_BLOCK 128
+#define HERO_FP8_SCALE_PITCH(columns) (((columns) + 511) / 512 * 4)
+
+/* x [n_rows, columns] (fp32 or bf16) in 8 bits: out_q [n_rows, columns], out_scales [ceil(n_rows / block_rows), pitch].
+ * block_rows: 1 (activations) or 128 (weights).  The buffers of an empty problem may be NULL. */
+int hero_quantize_fp8(const void* dev_x, int32_t x_dtype, int32_t n_rows, int32_t columns, int32_t block_rows,
+                      void* dev_out_q, void* dev_out_scales, void* stream);
+
+/* h = x[rows[i],:] (+ add[rows[i],:]); out row i = h * gain / sqrt(mean(h^2) + eps) in 8 bits [n_rows, hidden], scales
+ * [n_rows, pitch].  rows == NULL means rows[i] = i; rows may repeat.  add may be NULL.  With dev_sum row i of
+ * [n_rows, hidden], of x's type, is set to h: the residual's addition.  dev_sum may be dev_x itself where rows is NULL (each
+ * row is read before it is written), and overlaps no input otherwise.  The norm uses h before it is rounded for storage.  hidden a multiple
+ * of 16, <= 16384.  Statistics in fp32: h^2 and its sum have to stay below 3.4e38. */
+int hero_gather_rms_fp8(const void* dev_x, int32_t x_dtype, const void* dev_add_bf16, const int32_t* dev_rows,
+                        int32_t n_rows, int32_t hidden, const void* gain, float eps, void* dev_sum,
+                        void* dev_out_q, void* dev_out_scales, void* stream);
+
+/* C[M,N] = act(A[M,K] W[N,K]^T + bias[N]), A and W in 8 bits (A's scales [M, pitch(K)], W's [ceil(N/128), pitch(K)]), bias
+ * bf16 or NULL (none).  act as for hero_linear.  K and N multiples of 16.  hero_linear_fp8 stores C in bf16,
+ * hero_linear_fp8_quantized in 8 bits (out_q [M,N], out_scales [M, pitch(N)]), ready to be the next product's A.
+ * Products are added up in fp32; the matrix instructions align the products of eight neighbouring k to the largest of them,
+ * which keeps 13 bits below its leading one.
+ * Pointers 16-byte aligned (scales 4-byte).  (M + 512) * K and (N + 512) * K must stay below 2^32, else HERO_ERR_SHAPE.
+ * dev_scratch: optional (NULL and 0: none) device memory of the caller, 16-byte aligned, any contents, any size, as for
+ * hero_linear_scratch: some problems are faster with it.  Calls that share it must not overlap. */
+int hero_linear_fp8(const void* dev_a, const void* dev_a_scales, const void* dev_w, const void* dev_w_scales,
+                    const void* dev_bias, void* dev_c_bf16, int32_t m, int32_t n, int32_t k, int32_t act,
+                    void* dev_scratch, size_t scratch_bytes, void* stream);
+int hero_linear_fp8_quantized(const void* dev_a, const void* dev_a_scales, const void* dev_w, const void* dev_w_scales,
+                              const void* dev_bias, void* dev_out_q, void* dev_out_scales, int32_t m, int32_t n,
+                              int32_t k, int32_t act, void* dev_scratch, size_t scratch_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

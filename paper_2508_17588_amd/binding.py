@@ -46,6 +46,7 @@ EXPORTS = (
     "hero_attention", "hero_attention_scratch", "hero_attention_counted",
     "hero_axpy_features", "hero_second_diff_stats", "hero_stability_scores",
     "hero_linear_route", "hero_layer_route", "hero_attention_route",
+    "hero_quantize_fp8", "hero_gather_rms_fp8", "hero_linear_fp8", "hero_linear_fp8_quantized",
 )
 
 
@@ -115,6 +116,10 @@ def load_library(path: Optional[str] = None) -> ctypes.CDLL:
         "hero_linear_route": [I, I, I, I, I, ctypes.c_size_t, POINTER(I), POINTER(I), POINTER(I), POINTER(I)],
         "hero_layer_route": [POINTER(hero_config), I, I, I, POINTER(I), POINTER(I), POINTER(I), POINTER(I)],
         "hero_attention_route": [I, I, I, I, ctypes.c_size_t, POINTER(I), POINTER(I)],
+        "hero_quantize_fp8": [P, I, I, I, I, P, P, P],
+        "hero_gather_rms_fp8": [P, I, P, P, I, I, P, c_float, P, P, P, P],
+        "hero_linear_fp8": [P, P, P, P, P, P, I, I, I, I, P, ctypes.c_size_t, P],
+        "hero_linear_fp8_quantized": [P, P, P, P, P, P, P, I, I, I, I, P, ctypes.c_size_t, P],
     }
     for name, argtypes in sig.items():
         fn = getattr(lib, name)
@@ -440,3 +445,112 @@ def hero_stability_scores(variances):
     out = (ctypes.c_double * n)()
     _check(load_library().hero_stability_scores(v, n, out))
     return list(out)
+
+
+# ---- 8-bit linear layers ------------------------------------------------------------------
+# Elements are torch.float8_e4m3fn tensors [rows, columns], scales torch.float8_e8m0fnu tensors
+# [rows, fp8_scale_pitch(columns)] (a weight's: [ceil(rows / 128), ...]).
+
+FP8_BLOCK = 128
+
+
+def fp8_scale_pitch(columns: int) -> int:
+    """Bytes of the scales of a row: one for 128 columns, filled up to 32-bit words."""
+    return (columns + 511) // 512 * 4
+
+
+def empty_fp8(rows: int, columns: int, block_rows: int = 1, device="cuda"):
+    """(elements, scales), uninitialised, for `rows` rows (block_rows 128: of a weight)."""
+    import torch
+    return (torch.empty(rows, columns, dtype=torch.float8_e4m3fn, device=device),
+            torch.empty(-(-rows // block_rows), fp8_scale_pitch(columns), dtype=torch.float8_e8m0fnu, device=device))
+
+
+def _need_fp8(q, scales, rows: int, columns: int, block_rows: int, name: str):
+    import torch
+    _need(q, torch.float8_e4m3fn, name)
+    _need(scales, torch.float8_e8m0fnu, name + " scales")
+    if q.numel() < rows * columns or scales.numel() < -(-rows // block_rows) * fp8_scale_pitch(columns):
+        raise ValueError(f"{name} or its scales are too small")
+
+
+def _fp8_stream(*tensors) -> c_void_p:
+    """The current stream of the current device, on which all tensors have to lie."""
+    import torch
+    device = torch.cuda.current_device()
+    for t in tensors:
+        if t is not None and t.device.index != device:
+            raise ValueError(f"tensor on {t.device}, but the current device is cuda:{device}")
+    return _stream()
+
+
+def hero_quantize_fp8(x, q, scales, block_rows: int = 1):
+    """x [rows, columns] (float32 or bfloat16) in 8 bits; block_rows 128: as a weight."""
+    if x.dim() != 2 or not x.is_cuda or not x.is_contiguous():
+        raise TypeError("x must be a contiguous device tensor [rows, columns]")
+    if block_rows not in (1, FP8_BLOCK):
+        raise ValueError("block_rows must be 1 or 128")
+    rows, columns = x.shape
+    _need_fp8(q, scales, rows, columns, block_rows, "q")
+    _check(load_library().hero_quantize_fp8(_ptr(x), _dtype_code(x), rows, columns, block_rows, _ptr(q), _ptr(scales),
+                                            _fp8_stream(x, q, scales)))
+
+
+def hero_gather_rms_fp8(x, add, rows, n_rows: int, gain, eps: float, q, scales, sum=None):
+    """q, scales: (x + add)[rows] * gain / rms in 8 bits; sum (optional, x's type) takes (x + add)[rows] itself."""
+    import torch
+    hidden = x.shape[-1]
+    if not x.is_cuda or not x.is_contiguous():
+        raise TypeError("x must be a contiguous device tensor")
+    _need(gain, torch.bfloat16, "gain")
+    _need_fp8(q, scales, n_rows, hidden, 1, "q")
+    if add is not None:
+        _need(add, torch.bfloat16, "add")
+    if sum is not None:
+        _need(sum, x.dtype, "sum")
+    if rows is not None:
+        _need(rows, torch.int32, "rows")
+    if (gain.numel() != hidden or (add is not None and add.numel() != x.numel())
+            or (rows.numel() if rows is not None else x.numel() // hidden) < n_rows
+            or (sum is not None and sum.numel() < n_rows * hidden)):
+        raise ValueError("shape mismatch")
+    _check(load_library().hero_gather_rms_fp8(_ptr(x), _dtype_code(x), _ptr(add), _ptr(rows), n_rows, hidden, _ptr(gain), eps,
+                                              _ptr(sum), _ptr(q), _ptr(scales),
+                                              _fp8_stream(x, add, rows, gain, q, scales, sum)))
+
+
+def _linear_fp8_operands(a, a_scales, w, w_scales, bias, scratch):
+    import torch
+    if a.dim() != 2 or w.dim() != 2 or w.shape[1] != a.shape[1]:
+        raise ValueError("shape mismatch")
+    (m, k), n = a.shape, w.shape[0]
+    _need_fp8(a, a_scales, m, k, 1, "a")
+    _need_fp8(w, w_scales, n, k, FP8_BLOCK, "w")
+    if bias is not None:
+        _need(bias, torch.bfloat16, "bias")
+        if bias.numel() != n:
+            raise ValueError("shape mismatch")
+    if scratch is not None and not (scratch.is_cuda and scratch.is_contiguous()):
+        raise ValueError("scratch must be a contiguous device tensor")
+    return m, n, k, 0 if scratch is None else scratch.numel() * scratch.element_size()
+
+
+def hero_linear_fp8(a, a_scales, w, w_scales, bias, c, act: int = 0, scratch=None):
+    """c (bfloat16) = act(a w^T + bias); bias may be None, scratch is an optional contiguous device tensor."""
+    import torch
+    m, n, k, scratch_bytes = _linear_fp8_operands(a, a_scales, w, w_scales, bias, scratch)
+    _need(c, torch.bfloat16, "c")
+    if c.numel() < m * n:
+        raise ValueError("shape mismatch")
+    _check(load_library().hero_linear_fp8(_ptr(a), _ptr(a_scales), _ptr(w), _ptr(w_scales), _ptr(bias), _ptr(c), m, n, k, act,
+                                          _ptr(scratch), scratch_bytes,
+                                          _fp8_stream(a, a_scales, w, w_scales, bias, c, scratch)))
+
+
+def hero_linear_fp8_quantized(a, a_scales, w, w_scales, bias, q, scales, act: int = 0, scratch=None):
+    """hero_linear_fp8 with the result in 8 bits: q, scales are the `a`, `a_scales` of a next product."""
+    m, n, k, scratch_bytes = _linear_fp8_operands(a, a_scales, w, w_scales, bias, scratch)
+    _need_fp8(q, scales, m, n, 1, "q")
+    _check(load_library().hero_linear_fp8_quantized(_ptr(a), _ptr(a_scales), _ptr(w), _ptr(w_scales), _ptr(bias), _ptr(q),
+                                                    _ptr(scales), m, n, k, act, _ptr(scratch), scratch_bytes,
+                                                    _fp8_stream(a, a_scales, w, w_scales, bias, q, scales, scratch)))

@@ -1,0 +1,42 @@
+// Device-side helpers of the 8-bit kernels: e4m3 elements, E8M0 scales.
+#pragma once
+#include <type_traits>
+
+#include "hero_device.h"
+
+typedef int i32x8_t __attribute__((ext_vector_type(8)));
+
+constexpr uint32_t FP8_SCALE_ONE = 127;      // 2^0
+
+// |v|, or 0 for NaN and infinities, which do not count for a block's scale
+__device__ __forceinline__ float finite_size(float v) {
+  const float s = __builtin_fabsf(v);
+  return s < __builtin_inff() ? s : 0.f;
+}
+
+// largest of the 16 lanes that a block of 128 elements takes at 8 a lane
+__device__ __forceinline__ float max_of_16_lanes(float v) {
+  auto step = [](float x, auto CTRL) {
+    const int y = __builtin_amdgcn_update_dpp(0, __float_as_int(x), decltype(CTRL)::value, 0xf, 0xf, true);
+    return fmaxf(x, __int_as_float(y));
+  };
+  v = step(v, std::integral_constant<int, 0x128>{});     // row_ror: the row is rotated by 8, 4, 2, 1 lanes
+  v = step(v, std::integral_constant<int, 0x124>{});
+  v = step(v, std::integral_constant<int, 0x122>{});
+  return step(v, std::integral_constant<int, 0x121>{});
+}
+
+// Scale byte of a block whose largest finite magnitude is `largest`: 2^(byte - 127) is the least power of two with
+// largest <= 448 * 2^(byte - 127).  448 = 1.75 * 2^8, so the exponent is read off the bits: no division, no rounding.
+__device__ __forceinline__ uint32_t fp8_scale_of(float largest) {
+  const uint32_t u = __float_as_uint(largest);
+  const int byte = (int)(u >> 23) - 8 + ((u & 0x7FFFFFu) > 0x600000u ? 1 : 0);
+  return u == 0 ? FP8_SCALE_ONE : (uint32_t)max(byte, 0);
+}
+// 1 / scale; bytes that fp8_scale_of gives are at most 247
+__device__ __forceinline__ float fp8_inverse_scale(uint32_t byte) { return __uint_as_float((254u - byte) << 23); }
+
+// four values, already over their scale, as e4m3, round to nearest even (beyond 464 and NaN: NaN)
+__device__ __forceinline__ uint32_t pack_fp8x4(float a, float b, float c, float d) {
+  return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(c, d, __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false), true);
+}

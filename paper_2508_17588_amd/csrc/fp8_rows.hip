@@ -1,0 +1,197 @@
+// Rows and weights in 8 bits (e4m3 elements, a power-of-two scale for each block of 128), by themselves or out of a
+// root-mean-square norm that also adds the residual branch.
+//
+// A wave takes 512 neighbouring elements of a row at a time, eight a lane: 16 lanes hold a block, whose largest magnitude
+// they find with four lane rotations, and the four scale bytes of the piece are one 32-bit word.  Everything here is
+// bound by HBM: one pass, every byte read and written once.
+#include <type_traits>
+
+#include "fp8_device.h"
+#include "hero_kernels.h"
+
+namespace {
+
+constexpr int PIECE = 512;                // elements of a wave's piece: four blocks
+
+// A lane's eight elements (zeros past the end of the row) into out_q; the piece's scale word is stored by lane 0.
+__device__ __forceinline__ void store_piece(const float* v, uint8_t* q, bool in_row, uint8_t* scale_word, int lane) {
+  float largest = 0.f;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) largest = fmaxf(largest, finite_size(v[e]));
+  const uint32_t byte = fp8_scale_of(max_of_16_lanes(largest));
+  const float inv = fp8_inverse_scale(byte);
+  if (in_row) {
+    const u32x2_t out = {pack_fp8x4(v[0] * inv, v[1] * inv, v[2] * inv, v[3] * inv),
+                         pack_fp8x4(v[4] * inv, v[5] * inv, v[6] * inv, v[7] * inv)};
+    *reinterpret_cast<u32x2_t*>(q) = out;
+  }
+  uint32_t word = 0;
+#pragma unroll
+  for (int b = 0; b < 4; ++b) word |= (uint32_t)__builtin_amdgcn_readlane((int)byte, 16 * b) << (8 * b);
+  if (lane == 0) *reinterpret_cast<uint32_t*>(scale_word) = word;
+}
+
+// One wave a row for rows of up to 1024 elements (four rows to a workgroup), else one workgroup a row, ITERS pieces to each
+// of its WAVES waves, and the sum of squares goes through LDS.
+template <typename XT, int ITERS, int WAVES>
+__global__ __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES) void rms_fp8_kernel(RmsFp8Args a, int pitch) {
+  __shared__ float red[WAVES];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int64_t r = WAVES == 1 ? (int64_t)blockIdx.x * 4 + wave : (int64_t)blockIdx.x;
+  if (r >= a.n_rows) return;
+  const int64_t src = a.rows ? (int64_t)a.rows[r] : r;
+  const XT* xr = static_cast<const XT*>(a.x) + src * a.hidden;
+  const bf16_t* ar = a.add ? a.add + src * a.hidden : nullptr;
+  const int first = (WAVES == 1 ? 0 : wave * ITERS) * PIECE;         // this wave's first element
+  float v[ITERS][8];
+  u32x4_t gain[ITERS];
+  float sq = 0.f;
+#pragma unroll
+  for (int it = 0; it < ITERS; ++it) {
+    const int c = first + it * PIECE + lane * 8;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[it][e] = 0.f;
+    gain[it] = u32x4_t{0u, 0u, 0u, 0u};
+    if (c < a.hidden) {
+      ResidIO<XT>::load8(xr + c, v[it]);
+      if (ar) {
+        float b[8];
+        ResidIO<bf16_t>::load8(ar + c, b);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[it][e] += b[e];
+      }
+      gain[it] = *reinterpret_cast<const u32x4_t*>(a.gain + c);
+    }
+  }
+#pragma unroll
+  for (int it = 0; it < ITERS; ++it)
+#pragma unroll
+    for (int e = 0; e < 8; ++e) sq += v[it][e] * v[it][e];
+  sq = wave_sum(sq);
+  if (WAVES > 1) {
+    if (lane == 0) red[wave] = sq;
+    __syncthreads();
+    sq = 0.f;
+#pragma unroll
+    for (int i = 0; i < WAVES; ++i) sq += red[i];
+  }
+  const float rstd = rsqrtf(sq / (float)a.hidden + a.eps);
+#pragma unroll
+  for (int it = 0; it < ITERS; ++it) {
+    const int piece = first + it * PIECE, c = piece + lane * 8;
+    if (piece >= a.hidden) break;
+    if (a.sum && c < a.hidden) ResidIO<XT>::store8(static_cast<XT*>(a.sum) + r * a.hidden + c, v[it]);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      v[it][2 * e] = v[it][2 * e] * rstd * unpack_lo(gain[it][e]);
+      v[it][2 * e + 1] = v[it][2 * e + 1] * rstd * unpack_hi(gain[it][e]);
+    }
+    // (past the end of a row the zeros may meet an infinite rstd)
+    if (c >= a.hidden) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[it][e] = 0.f;
+    }
+    store_piece(v[it], a.out.q + r * a.hidden + c, c < a.hidden, a.out.scales + r * pitch + piece / PIECE * 4, lane);
+  }
+}
+
+template <typename XT>
+__global__ __launch_bounds__(256) void quantize_rows_kernel(const XT* __restrict__ x, int64_t pieces, int columns,
+                                                            int row_pieces, Fp8Out out) {
+  const int lane = threadIdx.x & 63;
+  const int64_t p = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  if (p >= pieces) return;
+  const int64_t row = p / row_pieces;
+  const int i = (int)(p - row * row_pieces), c = i * PIECE + lane * 8;
+  float v[8];
+#pragma unroll
+  for (int e = 0; e < 8; ++e) v[e] = 0.f;
+  if (c < columns) ResidIO<XT>::load8(x + row * columns + c, v);
+  store_piece(v, out.q + row * columns + c, c < columns, out.scales + p * 4, lane);
+}
+
+// 128 x 128 blocks: a workgroup a block, 16 rows of it at a time, all of it in registers until its largest magnitude is known
+template <typename XT>
+__global__ __launch_bounds__(256) void quantize_blocks_kernel(const XT* __restrict__ x, int n_rows, int columns,
+                                                              int pitch, Fp8Out out) {
+  __shared__ float red[4];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int c = blockIdx.x * 128 + (threadIdx.x & 15) * 8, r0 = blockIdx.y * 128 + (threadIdx.x >> 4);
+  float v[8][8], largest = 0.f;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[i][e] = 0.f;
+    if (c < columns && r0 + 16 * i < n_rows) ResidIO<XT>::load8(x + (int64_t)(r0 + 16 * i) * columns + c, v[i]);
+  }
+#pragma unroll
+  for (int i = 0; i < 8; ++i)
+#pragma unroll
+    for (int e = 0; e < 8; ++e) largest = fmaxf(largest, finite_size(v[i][e]));
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) largest = fmaxf(largest, __shfl_xor(largest, o, 64));
+  if (lane == 0) red[wave] = largest;
+  __syncthreads();
+  largest = fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3]));
+  const uint32_t byte = fp8_scale_of(largest);
+  const float inv = fp8_inverse_scale(byte);
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    if (c >= columns || r0 + 16 * i >= n_rows) continue;
+    const float* t = v[i];
+    const u32x2_t o = {pack_fp8x4(t[0] * inv, t[1] * inv, t[2] * inv, t[3] * inv),
+                       pack_fp8x4(t[4] * inv, t[5] * inv, t[6] * inv, t[7] * inv)};
+    *reinterpret_cast<u32x2_t*>(out.q + (int64_t)(r0 + 16 * i) * columns + c) = o;
+  }
+  // the last block of a row of blocks also writes the bytes that fill the word
+  const int b = blockIdx.x + threadIdx.x;
+  if (threadIdx.x == 0 || (blockIdx.x == gridDim.x - 1 && b < pitch))
+    out.scales[(int64_t)blockIdx.y * pitch + b] = (uint8_t)(threadIdx.x == 0 ? byte : FP8_SCALE_ONE);
+}
+
+template <typename XT>
+hipError_t rms_dispatch(const RmsFp8Args& a, hipStream_t st) {
+  const int pieces = (a.hidden + PIECE - 1) / PIECE, pitch = fp8_scale_pitch(a.hidden);
+#define LAUNCH(I, W)                                                                                               \
+  hipLaunchKernelGGL((rms_fp8_kernel<XT, I, W>), dim3(W == 1 ? (a.n_rows + 3) / 4 : a.n_rows), dim3(W == 1 ? 256 : 64 * W), 0, \
+                     st, a, pitch)
+  if (pieces <= 1) LAUNCH(1, 1);
+  else if (pieces <= 2) LAUNCH(2, 1);
+  else if (pieces <= 4) LAUNCH(2, 2);
+  else if (pieces <= 6) LAUNCH(2, 3);
+  else if (pieces <= 8) LAUNCH(2, 4);
+  else if (pieces <= 12) LAUNCH(2, 6);
+  else if (pieces <= 16) LAUNCH(2, 8);
+  else if (pieces <= 32) LAUNCH(4, 8);
+  else return hipErrorInvalidValue;
+#undef LAUNCH
+  return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_gather_rms_fp8(const RmsFp8Args& a, hipStream_t st) {
+  if (a.n_rows <= 0) return hipSuccess;
+  if (a.hidden <= 0 || a.hidden % 16 != 0) return hipErrorInvalidValue;
+  return a.x_fp32 ? rms_dispatch<float>(a, st) : rms_dispatch<bf16_t>(a, st);
+}
+
+hipError_t launch_quantize_fp8(const void* x, bool x_fp32, int n_rows, int columns, int block_rows, const Fp8Out& out,
+                               hipStream_t st) {
+  if (n_rows <= 0 || columns <= 0) return hipSuccess;
+  if (columns % 16 != 0) return hipErrorInvalidValue;
+  if (block_rows == 1) {
+    const int row_pieces = (columns + PIECE - 1) / PIECE;
+    const int64_t pieces = (int64_t)n_rows * row_pieces, groups = (pieces + 3) / 4;
+    if (groups > 0x7fffffff) return hipErrorInvalidValue;
+    const dim3 grid((unsigned)groups);
+    if (x_fp32) hipLaunchKernelGGL(quantize_rows_kernel<float>, grid, dim3(256), 0, st, static_cast<const float*>(x), pieces, columns, row_pieces, out);
+    else hipLaunchKernelGGL(quantize_rows_kernel<bf16_t>, grid, dim3(256), 0, st, static_cast<const bf16_t*>(x), pieces, columns, row_pieces, out);
+    return hipGetLastError();
+  }
+  const dim3 grid((columns + 127) / 128, (n_rows + 127) / 128);
+  const int pitch = fp8_scale_pitch(columns);
+  if (x_fp32) hipLaunchKernelGGL(quantize_blocks_kernel<float>, grid, dim3(256), 0, st, static_cast<const float*>(x), n_rows, columns, pitch, out);
+  else hipLaunchKernelGGL(quantize_blocks_kernel<bf16_t>, grid, dim3(256), 0, st, static_cast<const bf16_t*>(x), n_rows, columns, pitch, out);
+  return hipGetLastError();
+}

@@ -43,6 +43,9 @@ bool aligned16(std::initializer_list<const void*> ptrs) {
   return true;
 }
 
+// 512-element pieces of rows are counted in 31 bits
+bool fp8_rows_fit(int64_t n_rows, int64_t columns) { return n_rows * ((columns + 511) / 512) < (int64_t)1 << 31; }
+
 // ---- scratch owned by the library, for the entry point that must not allocate -----------------
 // Every device the library runs on holds its own copy of this array, at its own address, until
 // the process ends.  In host code the array's name is only a handle for hipGetSymbolAddress: the
@@ -1076,6 +1079,90 @@ int hero_axpy_features(void* dev_x, int32_t x_dtype, const void* s_cur, const vo
   HIP_TRY(launch_axpy_features(dev_x, x_dtype == HERO_DTYPE_FP32, (const bf16_t*)s_cur, (const bf16_t*)s_prev, alpha,
                                n_elems, (hipStream_t)stream));
   return HERO_OK;
+}
+
+// ---- 8-bit linear layers -----------------------------------------------------------
+
+int hero_quantize_fp8(const void* dev_x, int32_t x_dtype, int32_t n_rows, int32_t columns, int32_t block_rows,
+                      void* dev_out_q, void* dev_out_scales, void* stream) {
+  if (n_rows < 0) return fail(HERO_ERR_INVALID_ARG, "n_rows < 0");
+  if (n_rows > 0 && (!dev_x || !dev_out_q || !dev_out_scales)) return fail(HERO_ERR_INVALID_ARG, "null pointer");
+  if (x_dtype != HERO_DTYPE_FP32 && x_dtype != HERO_DTYPE_BF16) return fail(HERO_ERR_INVALID_ARG, "bad x_dtype");
+  if (block_rows != 1 && block_rows != HERO_FP8_BLOCK) return fail(HERO_ERR_INVALID_ARG, "block_rows must be 1 or 128");
+  if (columns < 16 || columns % 16 != 0) return fail(HERO_ERR_SHAPE, "columns must be a multiple of 16");
+  if (!fp8_rows_fit(n_rows, columns)) return fail(HERO_ERR_SHAPE, "n_rows * ceil(columns / 512) must stay below 2^31");
+  if (!aligned16({dev_x, dev_out_q}) || ((uintptr_t)dev_out_scales & 3))
+    return fail(HERO_ERR_INVALID_ARG, "x and out_q must be 16-byte aligned, out_scales 4-byte aligned");
+  HIP_TRY(launch_quantize_fp8(dev_x, x_dtype == HERO_DTYPE_FP32, n_rows, columns, block_rows,
+                              {(uint8_t*)dev_out_q, (uint8_t*)dev_out_scales}, (hipStream_t)stream));
+  return HERO_OK;
+}
+
+int hero_gather_rms_fp8(const void* dev_x, int32_t x_dtype, const void* dev_add_bf16, const int32_t* dev_rows,
+                        int32_t n_rows, int32_t hidden, const void* gain, float eps, void* dev_sum,
+                        void* dev_out_q, void* dev_out_scales, void* stream) {
+  if (n_rows < 0) return fail(HERO_ERR_INVALID_ARG, "n_rows < 0");
+  if (!gain || (n_rows > 0 && (!dev_x || !dev_out_q || !dev_out_scales))) return fail(HERO_ERR_INVALID_ARG, "null pointer");
+  if (x_dtype != HERO_DTYPE_FP32 && x_dtype != HERO_DTYPE_BF16) return fail(HERO_ERR_INVALID_ARG, "bad x_dtype");
+  if (!(eps >= 0.f)) return fail(HERO_ERR_INVALID_ARG, "eps must not be negative");
+  if (hidden < 16 || hidden % 16 != 0 || hidden > 16384) return fail(HERO_ERR_SHAPE, "hidden must be a multiple of 16, <= 16384");
+  if (!aligned16({dev_x, dev_add_bf16, gain, dev_sum, dev_out_q}) || ((uintptr_t)dev_rows & 3) || ((uintptr_t)dev_out_scales & 3))
+    return fail(HERO_ERR_INVALID_ARG, "x, add, gain, sum and out_q must be 16-byte aligned, rows and out_scales 4-byte aligned");
+  if (dev_sum && dev_rows && dev_sum == dev_x)
+    return fail(HERO_ERR_INVALID_ARG, "sum cannot be x itself where rows are listed: other rows may still be read");
+  if (dev_sum && !dev_rows && dev_sum != dev_x) {
+    const uintptr_t bytes = (uintptr_t)n_rows * hidden * (x_dtype == HERO_DTYPE_FP32 ? 4 : 2), d = (uintptr_t)dev_sum - (uintptr_t)dev_x;
+    if (d < bytes || 0 - d < bytes) return fail(HERO_ERR_INVALID_ARG, "sum may be x itself, but not overlap it otherwise");
+  }
+  RmsFp8Args a;
+  a.x = dev_x; a.x_fp32 = x_dtype == HERO_DTYPE_FP32; a.add = (const bf16_t*)dev_add_bf16; a.rows = dev_rows;
+  a.n_rows = n_rows; a.hidden = hidden; a.gain = (const bf16_t*)gain; a.eps = eps; a.sum = dev_sum;
+  a.out = {(uint8_t*)dev_out_q, (uint8_t*)dev_out_scales};
+  HIP_TRY(launch_gather_rms_fp8(a, (hipStream_t)stream));
+  return HERO_OK;
+}
+
+static int linear_fp8(GemmFp8Args& g, int32_t act, size_t scratch_bytes, hipStream_t st) {
+  if (g.m < 0 || g.n <= 0 || g.k <= 0) return fail(HERO_ERR_INVALID_ARG, "bad sizes");
+  if (!g.w || !g.w_scales || (g.m > 0 && (!g.a || !g.a_scales || !(g.c || (g.out.q && g.out.scales)))))
+    return fail(HERO_ERR_INVALID_ARG, "null pointer");
+  if (g.k % 16 != 0 || g.n % 16 != 0) return fail(HERO_ERR_SHAPE, "k and n must be multiples of 16");
+  if (act != 0 && act != 1) return fail(HERO_ERR_INVALID_ARG, "act must be 0 or 1");
+  if (((int64_t)g.m + 512) * g.k >= (int64_t)1 << 32 || ((int64_t)g.n + 512) * g.k >= (int64_t)1 << 32)
+    return fail(HERO_ERR_SHAPE, "(m + 512) * k and (n + 512) * k must stay below 2^32 (32-bit operand offsets)");
+  if (!aligned16({g.a, g.w, g.bias, g.c, g.out.q, g.scratch}) || (((uintptr_t)g.a_scales | (uintptr_t)g.w_scales | (uintptr_t)g.out.scales) & 3))
+    return fail(HERO_ERR_INVALID_ARG, "a, w, bias, the result and scratch must be 16-byte aligned, scales 4-byte aligned");
+  g.gelu = act != 0;
+  g.scratch_bytes = g.scratch ? scratch_bytes : 0;
+  HIP_TRY(launch_gemm_fp8(g, st));
+  return HERO_OK;
+}
+
+static GemmFp8Args fp8_operands(const void* dev_a, const void* dev_a_scales, const void* dev_w, const void* dev_w_scales,
+                                const void* dev_bias, int32_t m, int32_t n, int32_t k, void* dev_scratch) {
+  GemmFp8Args g;
+  g.a = (const uint8_t*)dev_a; g.a_scales = (const uint8_t*)dev_a_scales;
+  g.w = (const uint8_t*)dev_w; g.w_scales = (const uint8_t*)dev_w_scales;
+  g.bias = (const bf16_t*)dev_bias;
+  g.m = m; g.n = n; g.k = k;
+  g.scratch = (float*)dev_scratch;
+  return g;
+}
+
+int hero_linear_fp8(const void* dev_a, const void* dev_a_scales, const void* dev_w, const void* dev_w_scales,
+                    const void* dev_bias, void* dev_c_bf16, int32_t m, int32_t n, int32_t k, int32_t act,
+                    void* dev_scratch, size_t scratch_bytes, void* stream) {
+  GemmFp8Args g = fp8_operands(dev_a, dev_a_scales, dev_w, dev_w_scales, dev_bias, m, n, k, dev_scratch);
+  g.c = (bf16_t*)dev_c_bf16;
+  return linear_fp8(g, act, scratch_bytes, (hipStream_t)stream);
+}
+
+int hero_linear_fp8_quantized(const void* dev_a, const void* dev_a_scales, const void* dev_w, const void* dev_w_scales,
+                              const void* dev_bias, void* dev_out_q, void* dev_out_scales, int32_t m, int32_t n,
+                              int32_t k, int32_t act, void* dev_scratch, size_t scratch_bytes, void* stream) {
+  GemmFp8Args g = fp8_operands(dev_a, dev_a_scales, dev_w, dev_w_scales, dev_bias, m, n, k, dev_scratch);
+  g.out = {(uint8_t*)dev_out_q, (uint8_t*)dev_out_scales};
+  return linear_fp8(g, act, scratch_bytes, (hipStream_t)stream);
 }
 
 int hero_second_diff_stats(const void* f_prev, const void* f_cur, const void* f_next, int64_t n_elems,

@@ -192,3 +192,41 @@ struct AttnArgs {
 hipError_t launch_attention(const AttnArgs& a, hipStream_t st);
 // queries per workgroup of the kernel launch_attention takes, and the key ranges of the last round's blocks (1: not cut)
 void attention_route(const AttnArgs& a, int* queries, int* key_ranges);
+
+// 8-bit rows and weights: e4m3 elements, one E8M0 scale a block of 128 (include/hero.h)
+constexpr int fp8_scale_pitch(int columns) { return (columns + 511) / 512 * 4; }
+
+struct Fp8Out {
+  uint8_t* q = nullptr;            // [rows, columns]
+  uint8_t* scales = nullptr;       // [rows (or blocks of 128 rows), fp8_scale_pitch(columns)]
+};
+hipError_t launch_quantize_fp8(const void* x, bool x_fp32, int n_rows, int columns, int block_rows, const Fp8Out& out,
+                               hipStream_t st);
+
+struct RmsFp8Args {
+  const void* x = nullptr;
+  bool x_fp32 = false;
+  const bf16_t* add = nullptr;     // nullptr: none
+  const int32_t* rows = nullptr;   // nullptr: row i
+  int32_t n_rows = 0, hidden = 0;
+  const bf16_t* gain = nullptr;
+  float eps = 0.f;
+  void* sum = nullptr;             // x's type, row i; nullptr: not stored
+  Fp8Out out;
+};
+hipError_t launch_gather_rms_fp8(const RmsFp8Args& a, hipStream_t st);
+
+struct GemmFp8Args {
+  const uint8_t* a = nullptr;         // [m, k]
+  const uint8_t* a_scales = nullptr;  // [m, fp8_scale_pitch(k)]
+  const uint8_t* w = nullptr;         // [n, k]
+  const uint8_t* w_scales = nullptr;  // [ceil(n / 128), fp8_scale_pitch(k)]
+  const bf16_t* bias = nullptr;       // [n]; nullptr: none
+  int32_t m = 0, n = 0, k = 0;
+  bool gelu = false;
+  bf16_t* c = nullptr;                // [m, n], or:
+  Fp8Out out;                         // [m, n] in 8 bits
+  float* scratch = nullptr;           // optional, for partial sums along k (nullptr: never split)
+  size_t scratch_bytes = 0;
+};
+hipError_t launch_gemm_fp8(const GemmFp8Args& g, hipStream_t st);
