@@ -161,9 +161,16 @@ def test_rms_adds_the_branch_in_place(dtype):
 def operands(m, n, k, seed=0, bias=True):
     a = normal(seed + 1, m, k) * torch.exp2(torch.randint(-3, 4, (m, 1), generator=torch.Generator().manual_seed(seed)).float())
     a[:, k // 2] *= 30.0
-    ac, ab = F.quantized(a.double())
-    wc, wb = F.quantized(normal(seed + 2, n, k, scale=k ** -0.5).double(), 128)
-    return F.to_device(ac, ab), F.to_device(wc, wb), normal(seed + 3, n, scale=0.5, dtype=torch.bfloat16).cuda() if bias else None
+    w = normal(seed + 2, n, k, scale=k ** -0.5)
+    if m * k + n * k > 1 << 22:                    # (the plain quantiser walks over its blocks)
+        pairs = []
+        for t, block_rows in ((a, 1), (w, 128)):
+            pairs.append(B.empty_fp8(*t.shape, block_rows))
+            B.hero_quantize_fp8(t.cuda(), *pairs[-1], block_rows)
+        pairs = tuple(pairs)
+    else:
+        pairs = F.to_device(*F.quantized(a.double())), F.to_device(*F.quantized(w.double(), 128))
+    return pairs[0], pairs[1], normal(seed + 3, n, scale=0.5, dtype=torch.bfloat16).cuda() if bias else None
 
 
 def run_linear(a, w, bias, act, quantized, scratch=None, rows=None, spare=2):
@@ -205,6 +212,30 @@ def test_linear(m, n, k, quantized):
     say(f"linear {m} x {n} x {k} quantized {quantized}")
     a, w, bias = operands(m, n, k, seed=m + n + k)
     run_linear(a, w, bias, (m + n) % 2, quantized)
+
+
+# long k: several groups of scale words, tiles cut along k (scratch) or not
+LONG = [(300, 272, 4112), (256, 528, 6160), (130, 144, 8208), (4, 64, 5008), (70, 128, 4096)]
+
+
+@pytest.mark.parametrize("m,n,k", LONG)
+@pytest.mark.parametrize("quantized", [False, True])
+def test_linear_long_k(m, n, k, quantized):
+    say(f"linear {m} x {n} x {k} quantized {quantized}")
+    a, w, bias = operands(m, n, k)
+    scratch = torch.full((64 << 18,), float("nan"), device="cuda")
+    outs = [run_linear(a, w, bias, 1, quantized, scratch=s) for s in (None, scratch, scratch[: 1 << 10], scratch)]
+    for o in zip(*outs) if quantized else [outs]:
+        assert torch.equal(o[1].view(torch.uint8), o[3].view(torch.uint8)), "two calls differ"
+
+
+@pytest.mark.parametrize("m,n,k", [(4485, 4112, 272), (9001, 1920, 144), (2900, 2064, 4128), (1755, 528, 640)])
+@pytest.mark.parametrize("quantized", [False, True])
+def test_linear_many_tiles(m, n, k, quantized):
+    say(f"linear {m} x {n} x {k} quantized {quantized}")
+    a, w, bias = operands(m, n, k)
+    rows = torch.unique(torch.cat([torch.randint(0, m, (150,), generator=torch.Generator().manual_seed(9)), torch.tensor([0, m - 1])]))
+    run_linear(a, w, bias, 0, quantized, scratch=torch.empty(64 << 20, dtype=torch.uint8, device="cuda"), rows=rows)
 
 
 @pytest.mark.parametrize("quantized", [False, True])
