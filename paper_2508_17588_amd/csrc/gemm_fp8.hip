@@ -15,80 +15,6 @@
 
 namespace {
 
-// One wave a workgroup, 32 rows x 128 columns, fragments straight from memory: right for every size.
-template <bool QUANT>
-__global__ __launch_bounds__(64) void gemm_fp8_direct_kernel(GemmFp8Args g) {
-  const int lane = threadIdx.x, lr = lane & 31, lh = lane >> 5;
-  const int n0 = blockIdx.x * 128, m0 = blockIdx.y * 32;
-  const __amdgpu_buffer_rsrc_t ra = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(g.a), 0, (uint32_t)g.m * (uint32_t)g.k, 0x00020000);
-  const __amdgpu_buffer_rsrc_t rw = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(g.w), 0, (uint32_t)g.n * (uint32_t)g.k, 0x00020000);
-  const int pitch = fp8_scale_pitch(g.k);
-  const uint8_t* sa = g.a_scales + (int64_t)min(m0 + lr, g.m - 1) * pitch;
-  const uint8_t* sw = g.w_scales + (int64_t)blockIdx.x * pitch;
-  auto frag = [&](__amdgpu_buffer_rsrc_t rs, int row, int k0) {
-    i32x8_t f;
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      const int k = k0 + 32 * lh + 16 * h;
-      const uint32_t off = k < g.k ? (uint32_t)row * (uint32_t)g.k + (uint32_t)k : 0xFFFFFFF0u;   // (past the buffer: zero)
-      const auto t = __builtin_amdgcn_raw_buffer_load_b128(rs, off, 0, 0);
-#pragma unroll
-      for (int e = 0; e < 4; ++e) f[4 * h + e] = (int)t[e];
-    }
-    return f;
-  };
-  floatx16_t acc[4];
-#pragma unroll
-  for (int j = 0; j < 4; ++j)
-#pragma unroll
-    for (int e = 0; e < 16; ++e) acc[j][e] = 0.f;
-  for (int k = 0; k < g.k; k += 64) {
-    const int scale_a = sa[k >> 7], scale_w = sw[k >> 7];
-    const i32x8_t a = frag(ra, m0 + lr, k);
-#pragma unroll
-    for (int j = 0; j < 4; ++j)
-      acc[j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(frag(rw, n0 + 32 * j + lr, k), a, acc[j], 0, 0, 0, scale_w, 0, scale_a);
-  }
-  const int m = m0 + lr;
-  float largest = 0.f;
-#pragma unroll
-  for (int j = 0; j < 4; ++j)
-#pragma unroll
-    for (int q = 0; q < 4; ++q) {
-      const int n = n0 + 32 * j + 8 * q + 4 * lh;
-      u32x2_t bias = {0u, 0u};
-      if (g.bias && n < g.n) bias = *reinterpret_cast<const u32x2_t*>(g.bias + n);
-      float* v = reinterpret_cast<float*>(&acc[j]) + 4 * q;
-      v[0] += unpack_lo(bias[0]); v[1] += unpack_hi(bias[0]);
-      v[2] += unpack_lo(bias[1]); v[3] += unpack_hi(bias[1]);
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        if (g.gelu) v[e] = gelu_tanh(v[e]);
-        largest = fmaxf(largest, n < g.n ? finite_size(v[e]) : 0.f);
-      }
-      if (!QUANT && m < g.m && n < g.n) {
-        const u32x2_t out = {pack_bf16x2_hw(v[0], v[1]), pack_bf16x2_hw(v[2], v[3])};
-        *reinterpret_cast<u32x2_t*>(g.c + (int64_t)m * g.n + n) = out;
-      }
-    }
-  if (!QUANT) return;
-  const uint32_t byte = fp8_scale_of(fmaxf(largest, __shfl_xor(largest, 32, 64)));
-  const float inv = fp8_inverse_scale(byte);
-  if (m >= g.m) return;
-#pragma unroll
-  for (int j = 0; j < 4; ++j)
-#pragma unroll
-    for (int q = 0; q < 4; ++q) {
-      const int n = n0 + 32 * j + 8 * q + 4 * lh;
-      const float* v = reinterpret_cast<const float*>(&acc[j]) + 4 * q;
-      if (n < g.n) *reinterpret_cast<uint32_t*>(g.out.q + (int64_t)m * g.n + n) = pack_fp8x4(v[0] * inv, v[1] * inv, v[2] * inv, v[3] * inv);
-    }
-  if (lh == 0) {
-    const int out_pitch = fp8_scale_pitch(g.n), last = blockIdx.x == gridDim.x - 1 ? out_pitch : (int)blockIdx.x + 1;
-    for (int b = blockIdx.x; b < last; ++b) g.out.scales[(int64_t)m * out_pitch + b] = (uint8_t)(b == (int)blockIdx.x ? byte : FP8_SCALE_ONE);
-  }
-}
-
 // ------------------------------------------------------------------------------------------
 // Large problems: 256 x 256 tile, eight waves (two per SIMD) of 64 x 128, K walked in stages of 128 (one scale block, one
 // 128-byte line per row) through LDS rings of three A slots and two W slots (all 160 KB of a CU) that are filled by direct
@@ -124,6 +50,14 @@ struct Split {
 // chunks begin on whole scale words
 __device__ __forceinline__ int chunk_begin(int chunk, int n_chunks, int n_stages) {
   return chunk == n_chunks ? n_stages : chunk * n_stages / n_chunks / 4 * 4;
+}
+
+// Scale words of a weight's block of rows are the same for a whole wave: scalar loads (word clamped to the row's last)
+__device__ __forceinline__ uint32_t weight_scale_word(const GemmFp8Args& g, int n, int pitch, int word) {
+  typedef const __attribute__((address_space(4))) uint32_t* scalar_t;
+  const uint32_t row = (uint32_t)min(n, g.n - 1) / 128u;
+  const uint64_t at = (uint64_t)g.w_scales + (uint64_t)(row * (uint32_t)pitch) + 4u * (uint32_t)min(word, pitch / 4 - 1);
+  return *(scalar_t)at;
 }
 
 // A wave's 64 x 128 sums, acc[i][j][4q+e] = C[mw + 32i + lr][nw + 32j + 8q + 4lh + e], to the result; region: LDS of this wave
@@ -243,15 +177,14 @@ __global__ __launch_bounds__(512) void gemm256_fp8_kernel(GemmFp8Args g, int til
   // ---- scale bytes: of rows wm0 + 32i + lr, and of the wave's columns ----
   const int pitch = fp8_scale_pitch(g.k);
   const __amdgpu_buffer_rsrc_t rsSA = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(g.a_scales), 0, (uint32_t)g.m * (uint32_t)pitch, 0x00020000);
-  const __amdgpu_buffer_rsrc_t rsSW = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(g.w_scales), 0, (uint32_t)((g.n + 127) / 128) * (uint32_t)pitch, 0x00020000);
-  const uint32_t offSA = (uint32_t)(m0 + wm0 + lr) * (uint32_t)pitch, offSW = (uint32_t)((n0 + wn0) / 128) * (uint32_t)pitch;
+  const uint32_t offSA = (uint32_t)(m0 + wm0 + lr) * (uint32_t)pitch;
   uint32_t wordA[2][WORDS], wordW[WORDS], nextA[2][WORDS], nextW[WORDS];
   auto ask_scales = [&](int stage) {
 #pragma unroll
     for (int w = 0; w < WORDS; ++w) {
       nextA[0][w] = __builtin_amdgcn_raw_buffer_load_b32(rsSA, offSA, stage + 4 * w, 0);
       nextA[1][w] = __builtin_amdgcn_raw_buffer_load_b32(rsSA, offSA + 32u * (uint32_t)pitch, stage + 4 * w, 0);
-      nextW[w] = __builtin_amdgcn_raw_buffer_load_b32(rsSW, offSW, stage + 4 * w, 0);
+      nextW[w] = weight_scale_word(g, n0 + wn0, pitch, stage / 4 + w);
     }
   };
 
@@ -307,7 +240,7 @@ __global__ __launch_bounds__(512) void gemm256_fp8_kernel(GemmFp8Args g, int til
 #pragma unroll
           for (int i = 0; i < 2; ++i)
             wordA[i][w] = w + 1 < WORDS ? __builtin_amdgcn_alignbit(wordA[i][w + 1], wordA[i][w], 8) : wordA[i][w] >> 8;
-          wordW[w] = w + 1 < WORDS ? __builtin_amdgcn_alignbit(wordW[w + 1], wordW[w], 8) : wordW[w] >> 8;
+          wordW[w] = w + 1 < WORDS ? (wordW[w] >> 8 | wordW[w + 1] << 24) : wordW[w] >> 8;
         }
       }
       const int s = y >> 3, u = y >> 1;
@@ -333,7 +266,7 @@ __global__ __launch_bounds__(512) void gemm256_fp8_kernel(GemmFp8Args g, int til
 #pragma unroll
     for (int w = 0; w < WORDS; ++w) {
       wordA[0][w] = nextA[0][w]; wordA[1][w] = nextA[1][w];
-      wordW[w] = __builtin_amdgcn_readfirstlane(nextW[w]);
+      wordW[w] = nextW[w];
       asm volatile("" : "+v"(wordA[0][w]), "+v"(wordA[1][w]));
     }
     if (t0 + GROUP < stage_end) ask_scales(t0 + GROUP);
@@ -413,6 +346,464 @@ hipError_t launch_gemm256_fp8(const GemmFp8Args& g, int split, hipStream_t st) {
 }
 
 
+// ------------------------------------------------------------------------------------------
+// Smaller problems.  Their kernels end in stream_tile, which takes the fp32 sums row by row.
+// ------------------------------------------------------------------------------------------
+
+// BM x BN sums at (m0, n0), eight neighbouring ones from load(row, column, v), to the result, by NT threads.  In 8 bits a row
+// of 128 columns lies in 16 neighbouring lanes, which find its scale (BN = 128, and whole rounds of all threads of a wave).
+template <bool QUANT, bool GELU, int BM, int BN, int NT, typename Load>
+__device__ __forceinline__ void stream_tile(const GemmFp8Args& g, int m0, int n0, int tid, Load load) {
+  constexpr int PIECES = BN / 8;
+  static_assert(!QUANT || (BN == 128 && BM * PIECES % 64 == 0), "a row's block lies in 16 lanes");
+  const int out_pitch = fp8_scale_pitch(g.n), block = n0 >> 7, blocks = (g.n + 127) >> 7;
+  const bf16_t* bias = g.bias != nullptr ? g.bias : reinterpret_cast<const bf16_t*>(g.w);   // (any readable place)
+  for (int p = tid; p < BM * PIECES; p += NT) {
+    const int ml = p / PIECES, nl = (p - ml * PIECES) * 8, m = m0 + ml, n = n0 + nl;
+    float v[8];
+    load(ml, nl, v);
+    u32x4_t b = *reinterpret_cast<const u32x4_t*>(bias + min(n, g.n - 8));
+    if (g.bias == nullptr) b = u32x4_t{0u, 0u, 0u, 0u};
+#pragma unroll
+    for (int e = 0; e < 4; ++e) { v[2 * e] += unpack_lo(b[e]); v[2 * e + 1] += unpack_hi(b[e]); }
+    if (GELU) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[e] = gelu_tanh(v[e]);
+    }
+    if (!QUANT) {
+      u32x4_t out;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) out[e] = pack_bf16x2_hw(v[2 * e], v[2 * e + 1]);
+      if (m < g.m && n < g.n) *reinterpret_cast<u32x4_t*>(g.c + (int64_t)m * g.n + n) = out;
+    } else {
+      float largest = 0.f;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) largest = fmaxf(largest, n < g.n ? finite_size(v[e]) : 0.f);
+      const uint32_t byte = fp8_scale_of(max_of_16_lanes(largest));
+      const float inv = fp8_inverse_scale(byte);
+      if (m < g.m && n < g.n) {
+        const u32x2_t out = {pack_fp8x4(v[0] * inv, v[1] * inv, v[2] * inv, v[3] * inv),
+                             pack_fp8x4(v[4] * inv, v[5] * inv, v[6] * inv, v[7] * inv)};
+        *reinterpret_cast<u32x2_t*>(g.out.q + (int64_t)m * g.n + n) = out;
+      }
+      if (m < g.m && nl == 0) {
+        uint8_t* s = g.out.scales + (int64_t)m * out_pitch;
+        s[block] = (uint8_t)byte;
+        if (block == blocks - 1)
+          for (int x = blocks; x < out_pitch; ++x) s[x] = (uint8_t)FP8_SCALE_ONE;
+      }
+    }
+  }
+}
+
+// Tiles of less than 256 x 256 cut along k: slots 0 .. full_items - 1 are whole work items, the `tiles` slots after them are cut
+// in `chunks`, whose sums ([BM][BN] floats a chunk) the fix-up kernel adds up.  All first chunks, then all second ones, ..., so
+// that the chunks of a tile stay on the XCD that owns its range of tiles (slots are a multiple of 8).
+struct Cut {
+  int32_t full_items, tiles, chunks;
+  float* parts;
+};
+struct CutItem { int slot, chunk, n_chunks; };
+__device__ __forceinline__ CutItem cut_item(const Cut& cut) {
+  const int r = (int)blockIdx.x - cut.full_items;
+  if (r < 0) return {(int)blockIdx.x, 0, 1};
+  return {cut.full_items + r % cut.tiles, r / cut.tiles, cut.chunks};
+}
+
+// BM x BN tile, eight waves: 2 x 2 sub-tiles, each computed by two waves that take one half of every stage of 128 k.  The
+// sub-tile is then large (few LDS reads a flop) with two waves on every SIMD.  Stages go global -> LDS into a ring of RING
+// slots, filled RING - 1 stages ahead, one barrier a stage; a slot holds the BM rows of A, then the BN rows of W.  As in the
+// 256 x 256 kernel the MFMAs of a stage's last W fragment run after the next barrier, while the first fragments arrive.
+template <int BM, int BN>
+struct HalfK {
+  static constexpr int STAGE = (BM + BN) * 128;                          // bytes
+  static constexpr int RING = 163840 / STAGE < 4 ? 163840 / STAGE : 4;
+  static constexpr int TILE_BYTES = BM * (BN + 4) * 4;
+  static constexpr int LDS = RING * STAGE > TILE_BYTES ? RING * STAGE : TILE_BYTES;
+  static constexpr int WORDS = BM <= 128 ? 6 : BM + BN <= 320 ? 4 : 2;   // scale words of a row that are held: what the registers allow
+};
+
+template <int BM, int BN, bool QUANT, bool GELU>
+__global__ __launch_bounds__(512) void gemm_fp8_halfk_kernel(GemmFp8Args g, int tiles_m, int tiles_n, int per_xcd, int group_m, Cut cut) {
+  using C = HalfK<BM, BN>;
+  constexpr int MB = BM / 64, NB = BN / 64;            // 32 x 32 blocks of a wave's BM/2 x BN/2 sub-tile
+  constexpr int NF = (BM + BN) / 64;                   // 1 KB fills of a wave per stage
+  constexpr int RING = C::RING, STAGE = C::STAGE, WORDS = C::WORDS, GROUP = 4 * WORDS;
+  constexpr int STEPS = MB * NB, NW = BN == 128 ? 1 : NB;              // scale blocks among a wave's columns
+  static_assert(BM % 64 == 0 && BN % 64 == 0 && RING >= 3 && NB >= 2, "tile shape");
+  const CutItem it = cut_item(cut);
+  int m0, n0;
+  if (!tile_origin(it.slot, BM, BN, tiles_m, tiles_n, per_xcd, group_m, m0, n0)) return;
+
+  extern __shared__ u32x4_t smem[];
+  const uint32_t lds0 = (uint32_t)(size_t)(__attribute__((address_space(3))) void*)smem;
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);             // waves w and w+4 share a SIMD
+  const int wm0 = (wave & 1) * (BM / 2), wn0 = ((wave >> 1) & 1) * (BN / 2), kg = wave >> 2;
+  const int lr = lane & 31, lh = lane >> 5;
+
+  // fills: this wave's blocks of eight rows are wave + 8i of the slot's (BM + BN) / 8
+  const uint32_t row_bytes = (uint32_t)g.k;
+  const u32x4_t rsA = rsrc_words(g.a, (uint32_t)g.m * row_bytes);
+  const u32x4_t rsB = rsrc_words(g.w, (uint32_t)g.n * row_bytes);
+  const int row = wave * 8 + (lane >> 3);
+  const uint32_t fill_chunk = (lane & 7) ^ ((row >> 1) & 7);
+  const uint32_t voffA = (uint32_t)(m0 + row) * row_bytes + fill_chunk * 16, voffB = (uint32_t)(n0 + row) * row_bytes + fill_chunk * 16;
+  const uint32_t step64 = 64u * row_bytes;
+  const int n_stages = (g.k + BK - 1) / BK;
+  const int stage_begin = chunk_begin(it.chunk, it.n_chunks, n_stages), stage_end = chunk_begin(it.chunk + 1, it.n_chunks, n_stages);
+  const uint32_t past = fill_chunk * 16 >= (uint32_t)(g.k - (n_stages - 1) * BK) ? 0xFFFFFFF0u : 0u;
+  auto fill = [&](int slot, int want, int i) {
+    const int stage = min(want, stage_end - 1);        // (past the end: the last stage again, unread)
+    const uint32_t v = i < BM / 64 ? voffA + (uint32_t)i * step64 : voffB + (uint32_t)(i - BM / 64) * step64;
+    lds_fill(i < BM / 64 ? rsA : rsB, lds0 + wave * 1024 + i * 8192 + (uint32_t)slot * STAGE, v | (stage == n_stages - 1 ? past : 0u),
+             (uint32_t)stage * BK);
+  };
+
+  const int pitch = fp8_scale_pitch(g.k);
+  const __amdgpu_buffer_rsrc_t rsSA = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(g.a_scales), 0, (uint32_t)g.m * (uint32_t)pitch, 0x00020000);
+  const uint32_t offSA = (uint32_t)(m0 + wm0 + lr) * (uint32_t)pitch;
+  uint32_t wordA[MB][WORDS], nextA[MB][WORDS], wordW[NW][WORDS], nextW[NW][WORDS];
+  auto ask_scales = [&](int stage) {
+#pragma unroll
+    for (int w = 0; w < WORDS; ++w) {
+#pragma unroll
+      for (int i = 0; i < MB; ++i) nextA[i][w] = __builtin_amdgcn_raw_buffer_load_b32(rsSA, offSA + 32u * i * (uint32_t)pitch, stage + 4 * w, 0);
+#pragma unroll
+      for (int j = 0; j < NW; ++j) nextW[j][w] = weight_scale_word(g, n0 + wn0 + 32 * j, pitch, stage / 4 + w);
+    }
+  };
+
+  uint32_t first = (uint32_t)(lr * 128 + ((lh ^ ((lr >> 1) & 7)) * 16)) ^ (uint32_t)(64 * kg);
+  const uint32_t baseA = lds0 + wm0 * 128, baseB = lds0 + (BM + wn0) * 128;
+  auto frag = [&](uint32_t base, int i) {
+    typedef const __attribute__((address_space(3))) u32x4_t* lds_t;
+    const u32x4_t lo = *(lds_t)(size_t)(first + base + i * 4096), hi = *(lds_t)(size_t)((first ^ 32u) + base + i * 4096);
+    return i32x8_t{(int)lo[0], (int)lo[1], (int)lo[2], (int)lo[3], (int)hi[0], (int)hi[1], (int)hi[2], (int)hi[3]};
+  };
+
+  floatx16_t acc[MB][NB];
+#pragma unroll
+  for (int i = 0; i < MB; ++i)
+#pragma unroll
+    for (int j = 0; j < NB; ++j)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.f;
+  i32x8_t fa[2][MB], fb[NB];
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+#pragma unroll
+    for (int i = 0; i < MB; ++i) fa[1][i][e] = fa[0][i][e] = 0;
+#pragma unroll
+    for (int j = 0; j < NB; ++j) fb[j][e] = 0;
+  }
+  int scaleA[MB], scaleW[NW];
+#pragma unroll
+  for (int i = 0; i < MB; ++i) scaleA[i] = (int)FP8_SCALE_ONE;
+#pragma unroll
+  for (int j = 0; j < NW; ++j) scaleW[j] = (int)FP8_SCALE_ONE;
+  auto mma = [&](int set, int x) {
+    const int i = x % MB, j = x / MB;
+    acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(fb[j], fa[set][i], acc[i][j], 0, 0, 0, scaleW[NW == 1 ? 0 : j], 0, scaleA[i]);
+  };
+  int slot = 0;
+  auto stage = [&](auto SET, int t) {
+    constexpr int P = decltype(SET)::value;
+    // all but the fills of the RING - 2 newest stages have landed: stage t is in LDS; every wave's fragment reads of stage
+    // t-1 are complete, so its slot can be filled again
+    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"((RING - 2) * NF) : "memory");
+    __builtin_amdgcn_sched_barrier(0);
+    asm volatile("" : "+v"(first));
+    const uint32_t so = (uint32_t)slot * STAGE;
+    const int refill = slot == 0 ? RING - 1 : slot - 1;
+#pragma unroll
+    for (int y = 0; y < STEPS; ++y) {
+      if (y < NF) fill(refill, t + RING - 1, y);
+      if (y == STEPS - 1) {
+#pragma unroll
+        for (int z = STEPS; z < NF; ++z) fill(refill, t + RING - 1, z);
+      }
+      if (y == MB) {
+#pragma unroll
+        for (int i = 0; i < MB; ++i) scaleA[i] = (int)wordA[i][0];
+#pragma unroll
+        for (int j = 0; j < NW; ++j) scaleW[j] = (int)wordW[j][0];
+#pragma unroll
+        for (int w = 0; w < WORDS; ++w) {
+#pragma unroll
+          for (int i = 0; i < MB; ++i) wordA[i][w] = w + 1 < WORDS ? __builtin_amdgcn_alignbit(wordA[i][w + 1], wordA[i][w], 8) : wordA[i][w] >> 8;
+#pragma unroll
+          for (int j = 0; j < NW; ++j) wordW[j][w] = w + 1 < WORDS ? (wordW[j][w] >> 8 | wordW[j][w + 1] << 24) : wordW[j][w] >> 8;
+        }
+      }
+      if (y < MB) fa[P][y] = frag(baseA + so, y);
+      if (y % MB == 0) fb[y / MB] = frag(baseB + so, y / MB);
+      if (y < MB) mma(P ^ 1, STEPS - MB + y);
+      else mma(P, y - MB);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    slot = slot == RING - 1 ? 0 : slot + 1;
+  };
+  ask_scales(stage_begin);
+#pragma unroll
+  for (int s = 0; s < RING - 1; ++s)
+#pragma unroll
+    for (int i = 0; i < NF; ++i) fill(s, stage_begin + s, i);
+  for (int t0 = stage_begin; t0 < stage_end; t0 += GROUP) {
+#pragma unroll
+    for (int w = 0; w < WORDS; ++w) {
+#pragma unroll
+      for (int i = 0; i < MB; ++i) {
+        wordA[i][w] = nextA[i][w];
+        asm volatile("" : "+v"(wordA[i][w]));
+      }
+#pragma unroll
+      for (int j = 0; j < NW; ++j) wordW[j][w] = nextW[j][w];
+    }
+    if (t0 + GROUP < stage_end) ask_scales(t0 + GROUP);
+    const int group_end = min(t0 + GROUP, stage_end);
+    for (int t = t0; t < group_end; t += 2) {
+      stage(std::integral_constant<int, 0>{}, t);
+      if (t + 1 < group_end) {
+        stage(std::integral_constant<int, 1>{}, t + 1);
+      } else {
+        // an odd number of stages: the next set to be read is the other one again
+#pragma unroll
+        for (int i = 0; i < MB; ++i) fa[1][i] = fa[0][i];
+      }
+    }
+  }
+#pragma unroll
+  for (int y = 0; y < MB; ++y) mma(1, STEPS - MB + y);
+
+  asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+  __syncthreads();                       // every wave is done with the ring, and no fill is in flight
+  float* tile = reinterpret_cast<float*>(smem);
+  constexpr int LDT = BN + 4;
+  float* mine = tile + (wm0 + lr) * LDT + wn0 + 4 * lh;
+#pragma unroll
+  for (int half = 0; half < 2; ++half) {
+    if (kg == half) {
+#pragma unroll
+      for (int i = 0; i < MB; ++i)
+#pragma unroll
+        for (int j = 0; j < NB; ++j)
+#pragma unroll
+          for (int q = 0; q < 4; ++q) {
+            floatx4_t* p = reinterpret_cast<floatx4_t*>(mine + 32 * i * LDT + 32 * j + 8 * q);
+            floatx4_t v = {acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]};
+            if (half == 1) {
+              const floatx4_t o = *p;
+#pragma unroll
+              for (int e = 0; e < 4; ++e) v[e] += o[e];
+            }
+            *p = v;
+          }
+    }
+    __syncthreads();
+  }
+  if (it.n_chunks > 1) {
+    float* part = cut.parts + ((size_t)(it.slot - cut.full_items) * it.n_chunks + it.chunk) * (BM * BN);
+    for (int p = tid; p < BM * BN / 4; p += 512)
+      *reinterpret_cast<floatx4_t*>(part + p * 4) = *reinterpret_cast<const floatx4_t*>(tile + p / (BN / 4) * LDT + p % (BN / 4) * 4);
+    return;
+  }
+  stream_tile<QUANT, GELU, BM, BN, 512>(g, m0, n0, tid, [&](int ml, int nl, float* v) { ResidIO<float>::load8(tile + ml * LDT + nl, v); });
+}
+
+// Adds up the chunks of cut tiles and stores the result; 16 rows of a tile to a workgroup.
+template <int BM, int BN, bool QUANT, bool GELU>
+__global__ __launch_bounds__(256) void gemm_fp8_fixup_kernel(GemmFp8Args g, int tiles_m, int tiles_n, int per_xcd, int group_m, Cut cut) {
+  constexpr int ROWS = 16;
+  const int tile = blockIdx.x / (BM / ROWS), r0 = blockIdx.x % (BM / ROWS) * ROWS;
+  int m0, n0;
+  if (!tile_origin(cut.full_items + tile, BM, BN, tiles_m, tiles_n, per_xcd, group_m, m0, n0)) return;
+  const float* part = cut.parts + (size_t)tile * cut.chunks * (BM * BN) + r0 * BN;
+  stream_tile<QUANT, GELU, ROWS, BN, 256>(g, m0 + r0, n0, threadIdx.x, [&](int ml, int nl, float* v) {
+    const float* p = part + ml * BN + nl;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = 0.f;
+#pragma unroll 4
+    for (int c = 0; c < cut.chunks; ++c) {
+      float w[8];
+      ResidIO<float>::load8(p + (size_t)c * (BM * BN), w);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[e] += w[e];
+    }
+  });
+}
+
+// Few rows: what counts is that the weight's bytes are all asked for at once.  A workgroup of eight waves has 16 * R rows and
+// 16 columns (8-bit results: 128, a block), v_mfma_scale_f32_16x16x128_f8f6f4 (A fragment: lane holds row lane%16 and a
+// quarter of 128 k; accumulator register i of a lane is row 4*(lane/16) + i, column lane%16).  Each wave has its own share
+// of k (8-bit results: its own 16 columns) and a ring of its own, so there is no barrier until the sums meet in LDS.
+template <int R, int RING>
+struct FewRows {
+  static constexpr int STAGE = (16 * R + 16) * 128;                       // bytes: the rows of A, then 16 of W
+  static constexpr int WAVE = RING * STAGE + (R + 1) * 1024;               // and scale bytes of 64 stages: of the rows of A, of W
+  static constexpr int LDS = 8 * WAVE;
+};
+constexpr int ROWS_STAGES = 60;      // most stages of a wave: 64, as its scale bytes begin on a whole word
+
+template <int R, int RING, bool QUANT, bool GELU>
+__global__ __launch_bounds__(512) void gemm_fp8_rows_kernel(GemmFp8Args g, int tiles_n) {
+  using C = FewRows<R, RING>;
+  constexpr int STAGE = C::STAGE, NF = 2 * R + 2, COLS = QUANT ? 128 : 16;
+  extern __shared__ u32x4_t smem[];
+  const int tid = threadIdx.x, lane = tid & 63, lr = lane & 15, lq = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int tile_n = blockIdx.x % tiles_n, m0 = blockIdx.x / tiles_n * (16 * R), n0 = tile_n * COLS;
+  const int wn0 = n0 + (QUANT ? wave * 16 : 0);
+  const uint32_t ring = __builtin_amdgcn_readfirstlane((uint32_t)(size_t)(__attribute__((address_space(3))) void*)smem) + wave * C::WAVE;
+  const uint32_t scales = ring + RING * STAGE;
+  const uint32_t row_bytes = (uint32_t)g.k;
+  const u32x4_t rsA = rsrc_words(g.a, (uint32_t)g.m * row_bytes);
+  const u32x4_t rsB = rsrc_words(g.w, (uint32_t)g.n * row_bytes);
+  const int n_stages = (g.k + BK - 1) / BK;
+  const int begin = QUANT ? 0 : wave * n_stages / 8, end = QUANT ? n_stages : (wave + 1) * n_stages / 8;
+  // scale bytes: lane l brings those of row l/4, stages 16 * (l%4) .. +15 from the word of `begin` on; W's one row in lanes 0-3
+  const int pitch = fp8_scale_pitch(g.k), scale_begin = begin & ~3;
+  {
+    const u32x4_t rsSA = rsrc_words(g.a_scales, (uint32_t)g.m * (uint32_t)pitch);
+    const u32x4_t rsSW = rsrc_words(g.w_scales, (uint32_t)((g.n + 127) / 128) * (uint32_t)pitch);
+    const uint32_t at = (uint32_t)(scale_begin + (lane & 3) * 16);
+#pragma unroll
+    for (int i = 0; i < R; ++i) lds_fill(rsSA, scales + i * 1024, (uint32_t)(m0 + 16 * i + (lane >> 2)) * (uint32_t)pitch + at);
+    lds_fill(rsSW, scales + R * 1024, lane < 4 ? (uint32_t)(wn0 / 128) * (uint32_t)pitch + at : 0xFFFFFFF0u);
+  }
+  auto fill = [&](int slot, int stage) {
+#pragma unroll
+    for (int i = 0; i < NF; ++i) {
+      const int row = i * 8 + (lane >> 3), chunk = (lane & 7) ^ ((row >> 1) & 7);
+      const uint32_t past = stage * BK + chunk * 16 >= g.k ? 0xFFFFFFF0u : 0u;
+      const uint32_t v = (uint32_t)(i < 2 * R ? m0 + row : wn0 + row - 16 * R) * row_bytes + chunk * 16;
+      lds_fill(i < 2 * R ? rsA : rsB, ring + (uint32_t)slot * STAGE + i * 1024, v | past, (uint32_t)stage * BK);
+    }
+  };
+  floatx4_t acc[R];
+#pragma unroll
+  for (int i = 0; i < R; ++i) acc[i] = floatx4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+  for (int s = 0; s < RING; ++s)
+    if (begin + s < end) fill(s, begin + s);
+  // chunks lq and lq + 4 of a row; both operands take k in this order
+  const uint32_t first = (uint32_t)(lr * 128 + ((lq ^ ((lr >> 1) & 7)) * 16));
+  typedef const __attribute__((address_space(3))) u32x4_t* lds_t;
+  typedef const __attribute__((address_space(3))) uint8_t* lds_byte_t;
+  auto frag = [&](uint32_t base) {
+    const u32x4_t lo = *(lds_t)(size_t)(base + first), hi = *(lds_t)(size_t)(base + (first ^ 64u));
+    return i32x8_t{(int)lo[0], (int)lo[1], (int)lo[2], (int)lo[3], (int)hi[0], (int)hi[1], (int)hi[2], (int)hi[3]};
+  };
+  int slot = 0;
+  for (int t = begin; t < end; ++t) {
+    // the fills of the stages after this one may still be in flight
+    const int newer = min(RING - 1, end - 1 - t);
+    if (newer == 3) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(3 * NF) : "memory");
+    else if (newer == 2) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(2 * NF) : "memory");
+    else if (newer == 1) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(NF) : "memory");
+    else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    static_assert(RING <= 4, "counts above");
+    const uint32_t base = ring + (uint32_t)slot * STAGE, s = scales + (uint32_t)(t - scale_begin);
+    const i32x8_t w = frag(base + 2048 * R);
+    const int scale_w = *(lds_byte_t)(size_t)(s + R * 1024);
+    i32x8_t a[R];
+    int scale_a[R];
+#pragma unroll
+    for (int i = 0; i < R; ++i) {
+      a[i] = frag(base + 2048 * i);
+      scale_a[i] = *(lds_byte_t)(size_t)(s + i * 1024 + lr * 64);
+    }
+    if (t + RING < end) {
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");                  // the slot has been read
+      __builtin_amdgcn_sched_barrier(0);
+      fill(slot, t + RING);
+    }
+#pragma unroll
+    for (int i = 0; i < R; ++i)
+      acc[i] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(w, a[i], acc[i], 0, 0, 0, scale_w, 0, scale_a[i]);
+    slot = slot == RING - 1 ? 0 : slot + 1;
+  }
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");                        // (a wave without stages has scale bytes on their way)
+  __syncthreads();                       // every wave has read its last stage: no fill is in flight
+  // acc[i][e] = C[m0 + 16i + lr][wn0 + 4lq + e]
+  float* tile = reinterpret_cast<float*>(smem);
+  constexpr int LDT = COLS + 4, COPIES = QUANT ? 1 : 8;
+  static_assert(COPIES * 16 * R * LDT * 4 <= C::LDS, "sums");
+#pragma unroll
+  for (int i = 0; i < R; ++i)
+    *reinterpret_cast<floatx4_t*>(tile + ((QUANT ? 0 : wave * 16 * R) + 16 * i + lr) * LDT + (QUANT ? wave * 16 : 0) + 4 * lq) = acc[i];
+  __syncthreads();
+  stream_tile<QUANT, GELU, 16 * R, COLS, 512>(g, m0, n0, tid, [&](int ml, int nl, float* v) {
+    ResidIO<float>::load8(tile + ml * LDT + nl, v);
+#pragma unroll
+    for (int c = 1; c < COPIES; ++c) {
+      float w[8];
+      ResidIO<float>::load8(tile + (c * 16 * R + ml) * LDT + nl, w);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[e] += w[e];
+    }
+  });
+}
+
+template <int R, int RING, bool QUANT, bool GELU>
+hipError_t launch_rows_ring(const GemmFp8Args& g, hipStream_t st) {
+  static std::atomic<uint64_t> lds_allowed{0};
+  constexpr int LDS = FewRows<R, RING>::LDS;
+  auto kern = gemm_fp8_rows_kernel<R, RING, QUANT, GELU>;
+  hipError_t e = allow_dynamic_lds(reinterpret_cast<const void*>(kern), LDS, lds_allowed);
+  if (e != hipSuccess) return e;
+  const int tiles_n = QUANT ? (g.n + 127) / 128 : g.n / 16, tiles_m = (g.m + 16 * R - 1) / (16 * R);
+  hipLaunchKernelGGL(kern, dim3(tiles_n * tiles_m), dim3(512), LDS, st, g, tiles_n);
+  return hipGetLastError();
+}
+// stages of the wave that has most
+int rows_stages(const GemmFp8Args& g) {
+  const int stages = (g.k + BK - 1) / BK;
+  return g.out.q ? stages : (stages + 7) / 8;
+}
+// Two slots a wave where they hold all its stages (two workgroups to a CU), else as many as the LDS takes
+template <int R, bool QUANT, bool GELU>
+hipError_t launch_rows(const GemmFp8Args& g, hipStream_t st) {
+  if (rows_stages(g) > ROWS_STAGES) return hipErrorInvalidValue;
+  return rows_stages(g) <= 2 ? launch_rows_ring<R, 2, QUANT, GELU>(g, st) : launch_rows_ring<R, R == 1 ? 4 : 2, QUANT, GELU>(g, st);
+}
+
+template <int BM, int BN, bool QUANT, bool GELU>
+hipError_t launch_halfk(const GemmFp8Args& g, int chunks, hipStream_t st) {
+  static std::atomic<uint64_t> lds_allowed{0};
+  auto kern = gemm_fp8_halfk_kernel<BM, BN, QUANT, GELU>;
+  hipError_t e = allow_dynamic_lds(reinterpret_cast<const void*>(kern), HalfK<BM, BN>::LDS, lds_allowed);
+  if (e != hipSuccess) return e;
+  const int tiles_m = (g.m + BM - 1) / BM, tiles_n = (g.n + BN - 1) / BN;
+  const int per_xcd = (tiles_m * tiles_n + 7) / 8, slots = per_xcd * 8;
+  const int group_m = (g.k >= 8192 || tiles_m <= 24) ? 4 : 8;
+  const int full = chunks > 1 ? slots / 256 * 256 : slots;
+  const Cut cut = {full, slots - full, chunks, g.scratch};
+  hipLaunchKernelGGL(kern, dim3(full + (slots - full) * chunks), dim3(512), (HalfK<BM, BN>::LDS), st, g, tiles_m, tiles_n, per_xcd, group_m, cut);
+  if (slots > full)
+    hipLaunchKernelGGL((gemm_fp8_fixup_kernel<BM, BN, QUANT, GELU>), dim3((slots - full) * (BM / 16)), dim3(256), 0, st, g, tiles_m, tiles_n, per_xcd, group_m, cut);
+  return hipGetLastError();
+}
+
+enum TileKind { TILE_16, TILE_32, TILE_128, TILE_192x128, TILE_192, TILE_256 };
+
+template <bool QUANT, bool GELU>
+hipError_t launch_kind(const GemmFp8Args& g, TileKind kind, int chunks, hipStream_t st) {
+  switch (kind) {
+    case TILE_16: return launch_rows<1, QUANT, GELU>(g, st);
+    case TILE_32: return launch_rows<2, QUANT, GELU>(g, st);
+    case TILE_128: return launch_halfk<128, 128, QUANT, GELU>(g, chunks, st);
+    case TILE_192x128: return launch_halfk<192, 128, QUANT, GELU>(g, chunks, st);
+    case TILE_192:
+      if constexpr (QUANT) return hipErrorInvalidValue;                  // a block of 128 columns would lie in two tiles
+      else return launch_halfk<192, 192, QUANT, GELU>(g, chunks, st);
+    case TILE_256: return launch_gemm256_fp8<QUANT, GELU>(g, chunks, st);
+  }
+  return hipErrorInvalidValue;
+}
+
+struct TileChoice { TileKind kind; int chunks; };
+
 // The chip runs 256 workgroups at a time: the tiles of a last, partly filled round are cut along k where that pays (the round
 // then takes ceil(n * s / 256) / s of a tile's time) and the sums fit the scratch.
 int choose_split(const GemmFp8Args& g) {
@@ -429,6 +820,13 @@ int choose_split(const GemmFp8Args& g) {
   return split;
 }
 
+TileChoice choose_tile(const GemmFp8Args& g) {
+  if (g.m <= 16 && rows_stages(g) <= ROWS_STAGES) return {TILE_16, 1};
+  if (g.m <= 32 && rows_stages(g) <= ROWS_STAGES) return {TILE_32, 1};
+  if (g.m <= 512) return {TILE_128, 1};
+  return {TILE_256, choose_split(g)};
+}
+
 }  // namespace
 
 hipError_t launch_gemm_fp8(const GemmFp8Args& g, hipStream_t st) {
@@ -436,13 +834,7 @@ hipError_t launch_gemm_fp8(const GemmFp8Args& g, hipStream_t st) {
   if (g.k <= 0 || g.k % 16 != 0 || g.n % 16 != 0) return hipErrorInvalidValue;
   // operands are addressed with 32-bit byte offsets
   if (((int64_t)g.m + 512) * g.k >= (int64_t)1 << 32 || ((int64_t)g.n + 512) * g.k >= (int64_t)1 << 32) return hipErrorInvalidValue;
-  if (g.m > 128) {
-    const int split = choose_split(g);
-    if (g.out.q) return g.gelu ? launch_gemm256_fp8<true, true>(g, split, st) : launch_gemm256_fp8<true, false>(g, split, st);
-    return g.gelu ? launch_gemm256_fp8<false, true>(g, split, st) : launch_gemm256_fp8<false, false>(g, split, st);
-  }
-  const dim3 grid((g.n + 127) / 128, (g.m + 31) / 32);
-  if (g.out.q) hipLaunchKernelGGL(gemm_fp8_direct_kernel<true>, grid, dim3(64), 0, st, g);
-  else hipLaunchKernelGGL(gemm_fp8_direct_kernel<false>, grid, dim3(64), 0, st, g);
-  return hipGetLastError();
+  const TileChoice t = choose_tile(g);
+  if (g.out.q) return g.gelu ? launch_kind<true, true>(g, t.kind, t.chunks, st) : launch_kind<true, false>(g, t.kind, t.chunks, st);
+  return g.gelu ? launch_kind<false, true>(g, t.kind, t.chunks, st) : launch_kind<false, false>(g, t.kind, t.chunks, st);
 }

@@ -215,7 +215,8 @@ def test_linear(m, n, k, quantized):
 
 
 # long k: several groups of scale words, tiles cut along k (scratch) or not
-LONG = [(300, 272, 4112), (256, 528, 6160), (130, 144, 8208), (4, 64, 5008), (70, 128, 4096)]
+LONG = [(300, 272, 4112), (256, 528, 6160), (130, 144, 8208), (4, 64, 5008), (70, 128, 4096), (16, 48, 7696), (20, 272, 2064), (32, 144, 1936),
+        (1, 16, 70000), (2, 144, 8272)]
 
 
 @pytest.mark.parametrize("m,n,k", LONG)
