@@ -339,6 +339,7 @@ hipError_t launch_gemm256_fp8(const GemmFp8Args& g, int split, hipStream_t st) {
   const int group_m = (g.k >= 8192 || tiles_m <= 24) ? 4 : 8;
   const Split sk = {split > 1 ? slots / 256 * 256 : slots, split, g.scratch};
   const int cut = slots - sk.full_items;
+  if ((size_t)cut * sk.split * 262144 > (cut > 0 ? g.scratch_bytes : 0)) return hipErrorInvalidValue;
   hipLaunchKernelGGL(kern, dim3(sk.full_items + cut * sk.split), dim3(512), GEMM256_LDS, st, g, tiles_m, tiles_n, per_xcd, group_m, sk);
   if (cut > 0)
     hipLaunchKernelGGL((gemm256_fp8_fixup_kernel<QUANT, GELU>), dim3(cut * 8), dim3(64), STAGE_REGION, st, g, tiles_m, tiles_n, per_xcd, group_m, sk);
@@ -779,6 +780,7 @@ hipError_t launch_halfk(const GemmFp8Args& g, int chunks, hipStream_t st) {
   const int group_m = (g.k >= 8192 || tiles_m <= 24) ? 4 : 8;
   const int full = chunks > 1 ? slots / 256 * 256 : slots;
   const Cut cut = {full, slots - full, chunks, g.scratch};
+  if ((size_t)cut.tiles * chunks * (BM * BN * 4) > (cut.tiles > 0 ? g.scratch_bytes : 0)) return hipErrorInvalidValue;
   hipLaunchKernelGGL(kern, dim3(full + (slots - full) * chunks), dim3(512), (HalfK<BM, BN>::LDS), st, g, tiles_m, tiles_n, per_xcd, group_m, cut);
   if (slots > full)
     hipLaunchKernelGGL((gemm_fp8_fixup_kernel<BM, BN, QUANT, GELU>), dim3((slots - full) * (BM / 16)), dim3(256), 0, st, g, tiles_m, tiles_n, per_xcd, group_m, cut);
