@@ -32,11 +32,7 @@ namespace {
 constexpr int BK = 128;
 constexpr int STAGE_BYTES = 256 * BK;              // one operand, one stage: 32 KB
 constexpr int RING_B_OFF = 3 * STAGE_BYTES;        // the W ring starts after the A ring
-constexpr int CST = 272;                           // bf16 staging: bytes per 128-column row (+16 pad)
-constexpr int CST8 = 144;                          // 8-bit staging
-constexpr int STAGE_REGION = 64 * CST;             // per-wave staging region (17408 B)
 constexpr int GEMM256_LDS = 5 * STAGE_BYTES;
-static_assert(8 * STAGE_REGION <= GEMM256_LDS, "staging");
 constexpr int GROUP = 12;                          // stages whose scale bytes are held: a multiple of 6 (ring slots) and 4
 constexpr int WORDS = GROUP / 4;
 
@@ -60,36 +56,60 @@ __device__ __forceinline__ uint32_t weight_scale_word(const GemmFp8Args& g, int 
   return *(scalar_t)at;
 }
 
-// A wave's 64 x 128 sums, acc[i][j][4q+e] = C[mw + 32i + lr][nw + 32j + 8q + 4lh + e], to the result; region: LDS of this wave
+// Bias of 16 columns from n on (N is a multiple of 16), the same for a whole wave: scalar loads, which the vector memory
+// counter does not see; zeros past N and without bias
+struct Bias16 { uint32_t w[8]; };
+__device__ __forceinline__ Bias16 scalar_bias(const GemmFp8Args& g, int n) {
+  typedef const __attribute__((address_space(4))) uint32_t* scalar_t;
+  const bool have = g.bias != nullptr && n < g.n;
+  scalar_t p = (scalar_t)(g.bias == nullptr ? (uint64_t)g.w : (uint64_t)(g.bias + min(n, g.n - 16)));   // (any readable 32 bytes)
+  const uint32_t mask = have ? ~0u : 0u;
+  Bias16 b;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) b.w[e] = p[e] & mask;
+  return b;
+}
+
+// A wave's 64 x 128 sums, acc[i][j][4q+e] = C[m0 + wm0 + 32i + lr][nw + 32j + 8q + 4lh + e], to the result, staged in two
+// halves through 8 KB of this wave's LDS.  Every wave issues TILE_STORES<QUANT> stores or more, whatever lies outside the
+// matrix (the kernel counts on it): those go past the end of the buffer.
+template <bool QUANT> constexpr int TILE_STORES = QUANT ? 8 : 16;
+constexpr int STAGING = 8192;
 template <bool QUANT, bool GELU>
-__device__ __forceinline__ void store_tile(const GemmFp8Args& g, floatx16_t (&acc)[2][4], int mw, int nw, int lane, char* region) {
+__device__ __forceinline__ void store_tile(const GemmFp8Args& g, floatx16_t (&acc)[2][4], int m0, int wm0, int nw, int lane, char* region) {
   const int lr = lane & 31, lh = lane >> 5;
   const int out_pitch = fp8_scale_pitch(g.n), block = nw >> 7, blocks = (g.n + 127) >> 7;
-  const bf16_t* bias = g.bias != nullptr ? g.bias : reinterpret_cast<const bf16_t*>(g.w);   // (any readable place)
+  const uint32_t row_bytes = (uint32_t)g.n * (QUANT ? 1u : 2u);
+  char* base = (QUANT ? reinterpret_cast<char*>(g.out.q) : reinterpret_cast<char*>(g.c)) + (int64_t)m0 * row_bytes;
+  const uint32_t rows = (uint32_t)min(g.m - m0, 256);
+  const __amdgpu_buffer_rsrc_t rs = __builtin_amdgcn_make_buffer_rsrc(base, 0, rows * row_bytes, 0x00020000);
 #pragma unroll
   for (int i = 0; i < 2; ++i) {
     float largest = 0.f;
 #pragma unroll
     for (int j = 0; j < 4; ++j)
 #pragma unroll
-      for (int q = 0; q < 4; ++q) {
+      for (int h = 0; h < 2; ++h) {
         // (columns past N: no weights and no bias, so 0, which counts for no scale and is not stored)
-        const int n = nw + 32 * j + 8 * q + 4 * lh;
-        u32x2_t b = *reinterpret_cast<const u32x2_t*>(bias + min(n, g.n - 4));
-        if (g.bias == nullptr || n >= g.n) b = u32x2_t{0u, 0u};
-        float v[4] = {acc[i][j][4 * q] + unpack_lo(b[0]), acc[i][j][4 * q + 1] + unpack_hi(b[0]),
-                      acc[i][j][4 * q + 2] + unpack_lo(b[1]), acc[i][j][4 * q + 3] + unpack_hi(b[1])};
+        const Bias16 bias = scalar_bias(g, nw + 32 * j + 16 * h);
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          if (GELU) v[e] = gelu_tanh(v[e]);
-          if (QUANT) {
-            acc[i][j][4 * q + e] = v[e];
-            largest = fmaxf(largest, finite_size(v[e]));
+        for (int q2 = 0; q2 < 2; ++q2) {
+          const int q = 2 * h + q2;
+          const uint32_t b0 = lh ? bias.w[4 * q2 + 2] : bias.w[4 * q2], b1 = lh ? bias.w[4 * q2 + 3] : bias.w[4 * q2 + 1];
+          float v[4] = {acc[i][j][4 * q] + unpack_lo(b0), acc[i][j][4 * q + 1] + unpack_hi(b0),
+                        acc[i][j][4 * q + 2] + unpack_lo(b1), acc[i][j][4 * q + 3] + unpack_hi(b1)};
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            if (GELU) v[e] = gelu_tanh(v[e]);
+            if (QUANT) {
+              acc[i][j][4 * q + e] = v[e];
+              largest = fmaxf(largest, finite_size(v[e]));
+            }
           }
-        }
-        if (!QUANT) {
-          const u32x2_t pk = {pack_bf16x2_hw(v[0], v[1]), pack_bf16x2_hw(v[2], v[3])};
-          *reinterpret_cast<u32x2_t*>(region + (32 * i + lr) * CST + (32 * j + 8 * q + 4 * lh) * 2) = pk;
+          if (!QUANT) {
+            const u32x2_t pk = {pack_bf16x2_hw(v[0], v[1]), pack_bf16x2_hw(v[2], v[3])};
+            *reinterpret_cast<u32x2_t*>(region + lr * 256 + (((4 * j + q) ^ (lr & 15)) * 16) + lh * 8) = pk;
+          }
         }
       }
     if (QUANT) {
@@ -99,50 +119,55 @@ __device__ __forceinline__ void store_tile(const GemmFp8Args& g, floatx16_t (&ac
       for (int j = 0; j < 4; ++j)
 #pragma unroll
         for (int q = 0; q < 4; ++q)
-          *reinterpret_cast<uint32_t*>(region + (32 * i + lr) * CST8 + 32 * j + 8 * q + 4 * lh) =
+          *reinterpret_cast<uint32_t*>(region + lr * 128 + (((2 * j + (q >> 1)) ^ ((lr >> 1) & 7)) * 16) + (q & 1) * 8 + lh * 4) =
               pack_fp8x4(acc[i][j][4 * q] * inv, acc[i][j][4 * q + 1] * inv, acc[i][j][4 * q + 2] * inv, acc[i][j][4 * q + 3] * inv);
-      const int m = mw + 32 * i + lr;
+      const int m = m0 + wm0 + 32 * i + lr;
       if (lh == 0 && m < g.m && nw < g.n) {
         uint8_t* s = g.out.scales + (int64_t)m * out_pitch;
         s[block] = (uint8_t)byte;
         if (block == blocks - 1)
           for (int x = blocks; x < out_pitch; ++x) s[x] = (uint8_t)FP8_SCALE_ONE;
       }
+      // 32 rows x 8 pieces of 16 columns
+#pragma unroll
+      for (int it = 0; it < 4; ++it) {
+        const int rl = it * 8 + (lane >> 3), piece = lane & 7, n = nw + piece * 16;
+        const u32x4_t v = *reinterpret_cast<const u32x4_t*>(region + rl * 128 + ((piece ^ ((rl >> 1) & 7)) * 16));
+        __builtin_amdgcn_raw_buffer_store_b128(v, rs, n < g.n ? (uint32_t)(wm0 + 32 * i + rl) * row_bytes + (uint32_t)n : 0xFFFFFFF0u, 0, 0);
+      }
+    } else {
+      // 32 rows x 16 pieces of 8 columns: two 128-byte lines per row
+#pragma unroll
+      for (int it = 0; it < 8; ++it) {
+        const int rl = it * 4 + (lane >> 4), piece = lane & 15, n = nw + piece * 8;
+        const u32x4_t v = *reinterpret_cast<const u32x4_t*>(region + rl * 256 + ((piece ^ (rl & 15)) * 16));
+        __builtin_amdgcn_raw_buffer_store_b128(v, rs, n < g.n ? (uint32_t)(wm0 + 32 * i + rl) * row_bytes + (uint32_t)n * 2u : 0xFFFFFFF0u, 0, 0);
+      }
     }
     __builtin_amdgcn_sched_barrier(0);
-  }
-  if (!QUANT) {
-    // 64 rows x 16 pieces of 8 columns: two 128-byte lines per row
-#pragma unroll 4
-    for (int it = 0; it < 16; ++it) {
-      const int rl = it * 4 + (lane >> 4), piece = lane & 15;
-      const u32x4_t v = *reinterpret_cast<const u32x4_t*>(region + rl * CST + piece * 16);
-      const int m = mw + rl, n = nw + piece * 8;
-      if (m < g.m && n < g.n) *reinterpret_cast<u32x4_t*>(g.c + (int64_t)m * g.n + n) = v;
-    }
-  } else {
-    // 64 rows x 8 pieces of 16 columns
-#pragma unroll 4
-    for (int it = 0; it < 8; ++it) {
-      const int rl = it * 8 + (lane >> 3), piece = lane & 7;
-      const u32x4_t v = *reinterpret_cast<const u32x4_t*>(region + rl * CST8 + piece * 16);
-      const int m = mw + rl, n = nw + piece * 16;
-      if (m < g.m && n < g.n) *reinterpret_cast<u32x4_t*>(g.out.q + (int64_t)m * g.n + n) = v;
-    }
   }
 }
 
 template <bool QUANT, bool GELU>
 __global__ __launch_bounds__(512) void gemm256_fp8_kernel(GemmFp8Args g, int tiles_m, int tiles_n, int per_xcd, int group_m, Split sk) {
-  int slot = blockIdx.x, chunk = 0, n_chunks = 1;
-  if (slot >= sk.full_items) {
-    const int r = slot - sk.full_items;
-    slot = sk.full_items + r / sk.split;
-    chunk = r - (r / sk.split) * sk.split;
-    n_chunks = sk.split;
-  }
-  int m0, n0;
-  if (!tile_origin(slot, 256, 256, tiles_m, tiles_n, per_xcd, group_m, m0, n0)) return;
+  // ---- the work items of this workgroup: blockIdx.x, then every gridDim.x-th; a whole tile or a chunk of one ----
+  const int slots = 8 * per_xcd, n_items = sk.full_items + (slots - sk.full_items) * sk.split, n_stages = (g.k + BK - 1) / BK;
+  struct Item {
+    int index, m0, n0, part, begin, end;         // part: the chunk's place among the partial sums; -1: a whole tile
+  };
+  auto item_from = [&](int index) {              // the first one from `index` on that is a tile (some slots are empty)
+    for (; index < n_items; index += gridDim.x) {
+      const bool cut = index >= sk.full_items && sk.split > 1;
+      const int r = index - sk.full_items, slot = cut ? sk.full_items + r / sk.split : index, chunk = cut ? r % sk.split : 0;
+      int m0, n0;
+      if (tile_origin(slot, 256, 256, tiles_m, tiles_n, per_xcd, group_m, m0, n0))
+        return Item{index, m0, n0, cut ? r : -1, cut ? chunk_begin(chunk, sk.split, n_stages) : 0,
+                    cut ? chunk_begin(chunk + 1, sk.split, n_stages) : n_stages};
+    }
+    return Item{-1, 0, 0, -1, 0, 0};
+  };
+  Item it = item_from(blockIdx.x);
+  if (it.index < 0) return;
 
   extern __shared__ u32x4_t smem[];
   const uint32_t lds0 = (uint32_t)(size_t)(__attribute__((address_space(3))) void*)smem;
@@ -158,11 +183,9 @@ __global__ __launch_bounds__(512) void gemm256_fp8_kernel(GemmFp8Args g, int til
   const u32x4_t rsB = rsrc_words(g.w, (uint32_t)g.n * row_bytes);
   const int row = wave * 8 + (lane >> 3);
   const uint32_t fill_chunk = (lane & 7) ^ ((row >> 1) & 7);            // (the same for rows 64 apart)
-  const uint32_t voffA = (uint32_t)(m0 + row) * row_bytes + fill_chunk * 16, voffB = (uint32_t)(n0 + row) * row_bytes + fill_chunk * 16;
+  uint32_t voffA, voffB;
   const uint32_t step64 = 64u * row_bytes;
   const uint32_t fillA = lds0 + wave * 1024, fillB = lds0 + RING_B_OFF + wave * 1024;
-  const int n_stages = (g.k + BK - 1) / BK;
-  const int stage_begin = chunk_begin(chunk, n_chunks, n_stages), stage_end = chunk_begin(chunk + 1, n_chunks, n_stages);
   const uint32_t past = fill_chunk * 16 >= (uint32_t)(g.k - (n_stages - 1) * BK) ? 0xFFFFFFF0u : 0u;
   auto voff = [&](uint32_t base, int stage, int q) {
     return (base + (uint32_t)q * step64) | (stage == n_stages - 1 ? past : 0u);
@@ -177,14 +200,24 @@ __global__ __launch_bounds__(512) void gemm256_fp8_kernel(GemmFp8Args g, int til
   // ---- scale bytes: of rows wm0 + 32i + lr, and of the wave's columns ----
   const int pitch = fp8_scale_pitch(g.k);
   const __amdgpu_buffer_rsrc_t rsSA = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(g.a_scales), 0, (uint32_t)g.m * (uint32_t)pitch, 0x00020000);
-  const uint32_t offSA = (uint32_t)(m0 + wm0 + lr) * (uint32_t)pitch;
   uint32_t wordA[2][WORDS], wordW[WORDS], nextA[2][WORDS], nextW[WORDS];
-  auto ask_scales = [&](int stage) {
+  auto ask_scales = [&](int m0, int n0, int stage) {
+    int l = lane;
+    asm volatile("" : "+v"(l));
+    const uint32_t at = (uint32_t)(m0 + wm0 + (l & 31)) * (uint32_t)pitch;
 #pragma unroll
     for (int w = 0; w < WORDS; ++w) {
-      nextA[0][w] = __builtin_amdgcn_raw_buffer_load_b32(rsSA, offSA, stage + 4 * w, 0);
-      nextA[1][w] = __builtin_amdgcn_raw_buffer_load_b32(rsSA, offSA + 32u * (uint32_t)pitch, stage + 4 * w, 0);
+      nextA[0][w] = __builtin_amdgcn_raw_buffer_load_b32(rsSA, at, stage + 4 * w, 0);
+      nextA[1][w] = __builtin_amdgcn_raw_buffer_load_b32(rsSA, at + 32u * (uint32_t)pitch, stage + 4 * w, 0);
       nextW[w] = weight_scale_word(g, n0 + wn0, pitch, stage / 4 + w);
+    }
+  };
+  auto take_scales = [&]() {               // (pinned here: waiting for them is waiting for every fill before them)
+#pragma unroll
+    for (int w = 0; w < WORDS; ++w) {
+      wordA[0][w] = nextA[0][w]; wordA[1][w] = nextA[1][w];
+      wordW[w] = nextW[w];
+      asm volatile("" : "+v"(wordA[0][w]), "+v"(wordA[1][w]));
     }
   };
 
@@ -200,36 +233,30 @@ __global__ __launch_bounds__(512) void gemm256_fp8_kernel(GemmFp8Args g, int til
   };
 
   floatx16_t acc[2][4];
-#pragma unroll
-  for (int i = 0; i < 2; ++i)
-#pragma unroll
-    for (int j = 0; j < 4; ++j)
-#pragma unroll
-      for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.f;
   i32x8_t fa[2][2], fb[4];
-#pragma unroll
-  for (int e = 0; e < 8; ++e) {
-    fa[1][0][e] = fa[1][1][e] = 0;
-#pragma unroll
-    for (int u = 0; u < 4; ++u) fb[u][e] = 0;
-  }
-  int scaleA[2] = {(int)FP8_SCALE_ONE, (int)FP8_SCALE_ONE}, scaleW = (int)FP8_SCALE_ONE;
+  int scaleA[2], scaleW;
   // MFMA x of a stage: W fragment x/2 (slice x/8), A fragment x%2
   auto mma = [&](int x) {
     const int i = x & 1, u = (x >> 1) & 7, j = u & 3;
     acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(fb[u & 3], fa[u >> 2][i], acc[i][j], 0, 0, 0, scaleW, 0, scaleA[i]);
   };
+  bool after_stores = false;               // the last item's stores lie between this one's first fills and the rest
   auto stage = [&](auto SLOT_A, auto SLOT_B, int t) {
     constexpr int SA = decltype(SLOT_A)::value, SB = decltype(SLOT_B)::value;
     // All but the four newest fills (A of stage t+1) have landed: A and W of stage t are in LDS, and every wave's reads of
     // stage t-1 are complete: its slots are free.
-    asm volatile("s_waitcnt vmcnt(4) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    if (SA == 0 && SB == 0 && after_stores) {
+      after_stores = false;
+      asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(4 + TILE_STORES<QUANT>) : "memory");
+    } else {
+      asm volatile("s_waitcnt vmcnt(4) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    }
     __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
     for (int y = 0; y < 16; ++y) {
       // (past the last stage it is fetched once more into the idle slot: in bounds, never read)
-      if (y < 4) fill_b(SB ^ 1, min(t + 1, stage_end - 1), y);
-      else if (y < 8) fill_a((SA + 2) % 3, min(t + 2, stage_end - 1), y - 4);
+      if (y < 4) fill_b(SB ^ 1, min(t + 1, it.end - 1), y);
+      else if (y < 8) fill_a((SA + 2) % 3, min(t + 2, it.end - 1), y - 4);
       if (y == 4) {
         // the stage's own scales: byte 0 of the words, which move down by one
 #pragma unroll
@@ -244,7 +271,8 @@ __global__ __launch_bounds__(512) void gemm256_fp8_kernel(GemmFp8Args g, int til
         }
       }
       const int s = y >> 3, u = y >> 1;
-      if ((y & 7) == 0) asm volatile("" : "+v"(first));     // (its sums are formed here again, not held through the loop)
+      // (what follows from these is formed here again and not held in registers through the loop)
+      if ((y & 7) == 0) asm volatile("" : "+v"(first), "+v"(voffA), "+v"(voffB));
       if ((y & 7) == 0) fa[s][0] = frag(baseA, s, SA, 0);
       if ((y & 1) == 0) fb[u & 3] = frag(baseB, s, SB, u & 3);
       if ((y & 7) == 1) fa[s][1] = frag(baseA, s, SA, 1);
@@ -252,53 +280,91 @@ __global__ __launch_bounds__(512) void gemm256_fp8_kernel(GemmFp8Args g, int til
       __builtin_amdgcn_sched_barrier(0);
     }
   };
-  ask_scales(stage_begin);
+  // what an item's main loop needs first: A and W of its first stage, A of the second
+  auto start_item = [&]() {
+    int l = lane;
+    asm volatile("" : "+v"(l));
+    const int row = wave * 8 + (l >> 3);
+    const uint32_t at = (uint32_t)row * row_bytes + (uint32_t)((l & 7) ^ ((row >> 1) & 7)) * 16u;
+    voffA = (uint32_t)it.m0 * row_bytes + at;
+    voffB = (uint32_t)it.n0 * row_bytes + at;
 #pragma unroll
-  for (int q = 0; q < 4; ++q) fill_a(0, stage_begin, q);
+    for (int q = 0; q < 4; ++q) fill_a(0, it.begin, q);
 #pragma unroll
-  for (int q = 0; q < 4; ++q) fill_b(0, stage_begin, q);
+    for (int q = 0; q < 4; ++q) fill_b(0, it.begin, q);
 #pragma unroll
-  for (int q = 0; q < 4; ++q) fill_a(1, min(stage_begin + 1, stage_end - 1), q);
+    for (int q = 0; q < 4; ++q) fill_a(1, min(it.begin + 1, it.end - 1), q);
+  };
   using I0 = std::integral_constant<int, 0>;
   using I1 = std::integral_constant<int, 1>;
   using I2 = std::integral_constant<int, 2>;
-  for (int t0 = stage_begin; t0 < stage_end; t0 += GROUP) {
-#pragma unroll
-    for (int w = 0; w < WORDS; ++w) {
-      wordA[0][w] = nextA[0][w]; wordA[1][w] = nextA[1][w];
-      wordW[w] = nextW[w];
-      asm volatile("" : "+v"(wordA[0][w]), "+v"(wordA[1][w]));
-    }
-    if (t0 + GROUP < stage_end) ask_scales(t0 + GROUP);
-    const int group_end = min(t0 + GROUP, stage_end);
-    for (int t = t0; t < group_end; t += 6) {
-      stage(I0{}, I0{}, t);
-      if (t + 1 < stage_end) stage(I1{}, I1{}, t + 1);
-      if (t + 2 < stage_end) stage(I2{}, I0{}, t + 2);
-      if (t + 3 < stage_end) stage(I0{}, I1{}, t + 3);
-      if (t + 4 < stage_end) stage(I1{}, I0{}, t + 4);
-      if (t + 5 < stage_end) stage(I2{}, I1{}, t + 5);
-    }
-  }
-#pragma unroll
-  for (int x = 12; x < 16; ++x) mma(x);
-
-  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-  if (n_chunks > 1) {
-    float* part = sk.ws + ((size_t)(slot - sk.full_items) * sk.split + chunk) * 65536 + tid * 4;
+  ask_scales(it.m0, it.n0, it.begin);
+  start_item();
+  take_scales();
+  for (;;) {
+    const Item next = item_from(it.index + gridDim.x);
 #pragma unroll
     for (int i = 0; i < 2; ++i)
 #pragma unroll
       for (int j = 0; j < 4; ++j)
 #pragma unroll
-        for (int q = 0; q < 4; ++q) {
-          floatx4_t v = {acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]};
-          *reinterpret_cast<floatx4_t*>(part + ((i * 4 + j) * 4 + q) * 2048) = v;
-        }
-    return;
+        for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.f;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      fa[0][0][e] = fa[0][1][e] = fa[1][0][e] = fa[1][1][e] = 0;
+#pragma unroll
+      for (int u = 0; u < 4; ++u) fb[u][e] = 0;
+    }
+    scaleA[0] = scaleA[1] = scaleW = (int)FP8_SCALE_ONE;
+    for (int t0 = it.begin;;) {
+      const int group_end = min(t0 + GROUP, it.end);
+      if (group_end < it.end) ask_scales(it.m0, it.n0, group_end);
+      else if (next.index >= 0) ask_scales(next.m0, next.n0, next.begin);
+      for (int t = t0; t < group_end; t += 6) {
+        stage(I0{}, I0{}, t);
+        if (t + 1 < group_end) stage(I1{}, I1{}, t + 1);
+        if (t + 2 < group_end) stage(I2{}, I0{}, t + 2);
+        if (t + 3 < group_end) stage(I0{}, I1{}, t + 3);
+        if (t + 4 < group_end) stage(I1{}, I0{}, t + 4);
+        if (t + 5 < group_end) stage(I2{}, I1{}, t + 5);
+      }
+      t0 = group_end;
+      if (t0 >= it.end) break;
+      take_scales();
+    }
+#pragma unroll
+    for (int x = 12; x < 16; ++x) mma(x);
+
+    // Every wave is done with the rings, and no fill is in flight.  The next item's first fills go out before this one's
+    // result is stored: they arrive, and the stores drain, behind other work.
+    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    const Item done = it;
+    it = next;
+    if (it.index >= 0) {
+      take_scales();
+      start_item();
+    }
+    int l = lane;
+    asm volatile("" : "+v"(l));            // (addresses are formed here, not held in registers through the loop)
+    if (done.part >= 0) {
+      float* part = sk.ws + (size_t)done.part * 65536 + wave * 256 + l * 4;
+#pragma unroll
+      for (int i = 0; i < 2; ++i)
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+#pragma unroll
+          for (int q = 0; q < 4; ++q) {
+            floatx4_t v = {acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]};
+            *reinterpret_cast<floatx4_t*>(part + ((i * 4 + j) * 4 + q) * 2048) = v;
+          }
+    } else {
+      // staging lies in the slots that the next item fills after its first barrier: the third of A, the second of W
+      char* region = reinterpret_cast<char*>(smem) + (wave < 4 ? 2 * STAGE_BYTES : RING_B_OFF) + wave * STAGING;
+      store_tile<QUANT, GELU>(g, acc, done.m0, wm0, done.n0 + wn0, l, region);
+    }
+    if (it.index < 0) return;
+    after_stores = true;
   }
-  __syncthreads();                       // every wave is done with the rings
-  store_tile<QUANT, GELU>(g, acc, m0 + wm0, n0 + wn0, lane, reinterpret_cast<char*>(smem) + wave * STAGE_REGION);
 }
 
 // Adds up the chunks of the cut tiles and stores the result: a one-wave workgroup to each 64 x 128 part of a tile.
@@ -325,7 +391,7 @@ __global__ __launch_bounds__(64) void gemm256_fp8_fixup_kernel(GemmFp8Args g, in
 #pragma unroll
       for (int e = 0; e < 4; ++e) acc[x >> 4][(x >> 2) & 3][4 * (x & 3) + e] += v[x][e];
   }
-  store_tile<QUANT, GELU>(g, acc, m0 + (wave & 3) * 64, n0 + (wave >> 2) * 128, lane, reinterpret_cast<char*>(smem));
+  store_tile<QUANT, GELU>(g, acc, m0, (wave & 3) * 64, n0 + (wave >> 2) * 128, lane, reinterpret_cast<char*>(smem));
 }
 
 template <bool QUANT, bool GELU>
@@ -340,9 +406,9 @@ hipError_t launch_gemm256_fp8(const GemmFp8Args& g, int split, hipStream_t st) {
   const Split sk = {split > 1 ? slots / 256 * 256 : slots, split, g.scratch};
   const int cut = slots - sk.full_items;
   if ((size_t)cut * sk.split * 262144 > (cut > 0 ? g.scratch_bytes : 0)) return hipErrorInvalidValue;
-  hipLaunchKernelGGL(kern, dim3(sk.full_items + cut * sk.split), dim3(512), GEMM256_LDS, st, g, tiles_m, tiles_n, per_xcd, group_m, sk);
+  hipLaunchKernelGGL(kern, dim3(std::min(sk.full_items + cut * sk.split, 256)), dim3(512), GEMM256_LDS, st, g, tiles_m, tiles_n, per_xcd, group_m, sk);
   if (cut > 0)
-    hipLaunchKernelGGL((gemm256_fp8_fixup_kernel<QUANT, GELU>), dim3(cut * 8), dim3(64), STAGE_REGION, st, g, tiles_m, tiles_n, per_xcd, group_m, sk);
+    hipLaunchKernelGGL((gemm256_fp8_fixup_kernel<QUANT, GELU>), dim3(cut * 8), dim3(64), STAGING, st, g, tiles_m, tiles_n, per_xcd, group_m, sk);
   return hipGetLastError();
 }
 
