@@ -40,3 +40,12 @@ __device__ __forceinline__ float fp8_inverse_scale(uint32_t byte) { return __uin
 __device__ __forceinline__ uint32_t pack_fp8x4(float a, float b, float c, float d) {
   return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(c, d, __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false), true);
 }
+
+// A value the compiler knows nothing of from here on: what follows from it is formed again where it is used, and not kept in
+// registers from before.  (The scalar form has no meaning to the host's pass.)
+template <typename T> __device__ __forceinline__ void forget(T& v) { asm volatile("" : "+v"(v)); }
+template <typename T> __device__ __forceinline__ void forget_scalar(T& v) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  asm volatile("" : "+s"(v));
+#endif
+}

@@ -56,28 +56,18 @@ __device__ __forceinline__ uint32_t weight_scale_word(const GemmFp8Args& g, int 
   return *(scalar_t)at;
 }
 
-// Bias of 16 columns from n on (N is a multiple of 16), the same for a whole wave: scalar loads, which the vector memory
-// counter does not see; zeros past N and without bias
-struct Bias16 { uint32_t w[8]; };
-__device__ __forceinline__ Bias16 scalar_bias(const GemmFp8Args& g, int n) {
-  typedef const __attribute__((address_space(4))) uint32_t* scalar_t;
-  const bool have = g.bias != nullptr && n < g.n;
-  scalar_t p = (scalar_t)(g.bias == nullptr ? (uint64_t)g.w : (uint64_t)(g.bias + min(n, g.n - 16)));   // (any readable 32 bytes)
-  const uint32_t mask = have ? ~0u : 0u;
-  Bias16 b;
-#pragma unroll
-  for (int e = 0; e < 8; ++e) b.w[e] = p[e] & mask;
-  return b;
+// Bias of a wave's 128 columns, two a lane; past the end of the buffer (columns past N, or no bias) zeros
+__device__ __forceinline__ uint32_t load_bias(const GemmFp8Args& g, int nw, int lane) {
+  const __amdgpu_buffer_rsrc_t rs = __builtin_amdgcn_make_buffer_rsrc(const_cast<bf16_t*>(g.bias), 0, g.bias != nullptr ? (uint32_t)g.n * 2u : 0u, 0x00020000);
+  return __builtin_amdgcn_raw_buffer_load_b32(rs, (uint32_t)(nw + 2 * lane) * 2u, 0, 0);
 }
 
 // A wave's 64 x 128 sums, acc[i][j][4q+e] = C[m0 + wm0 + 32i + lr][nw + 32j + 8q + 4lh + e], to the result, staged in two
-// halves through 8 KB of this wave's LDS.  Every wave issues TILE_STORES<QUANT> stores or more, whatever lies outside the
-// matrix (the kernel counts on it): those go past the end of the buffer.
-template <bool QUANT> constexpr int TILE_STORES = QUANT ? 8 : 16;
-constexpr int STAGING = 8192;
+// quarters (8-bit results: halves) through 4 KB of this wave's LDS.  What lies outside the matrix is sent past the end of the buffer.
+constexpr int STAGING = 4096;
 template <bool QUANT, bool GELU>
-__device__ __forceinline__ void store_tile(const GemmFp8Args& g, floatx16_t (&acc)[2][4], int m0, int wm0, int nw, int lane, char* region) {
-  const int lr = lane & 31, lh = lane >> 5;
+__device__ __forceinline__ void store_tile(const GemmFp8Args& g, floatx16_t (&acc)[2][4], uint32_t bias, int m0, int wm0, int nw,
+                                           int lane, char* region) {
   const int out_pitch = fp8_scale_pitch(g.n), block = nw >> 7, blocks = (g.n + 127) >> 7;
   const uint32_t row_bytes = (uint32_t)g.n * (QUANT ? 1u : 2u);
   char* base = (QUANT ? reinterpret_cast<char*>(g.out.q) : reinterpret_cast<char*>(g.c)) + (int64_t)m0 * row_bytes;
@@ -85,33 +75,45 @@ __device__ __forceinline__ void store_tile(const GemmFp8Args& g, floatx16_t (&ac
   const __amdgpu_buffer_rsrc_t rs = __builtin_amdgcn_make_buffer_rsrc(base, 0, rows * row_bytes, 0x00020000);
 #pragma unroll
   for (int i = 0; i < 2; ++i) {
+    forget(bias); forget(lane);            // (what follows from these is formed again, not held from the first half)
+    const int lr = lane & 31, lh = lane >> 5;
     float largest = 0.f;
 #pragma unroll
-    for (int j = 0; j < 4; ++j)
+    for (int j = 0; j < 4; ++j) {
 #pragma unroll
-      for (int h = 0; h < 2; ++h) {
+      for (int q = 0; q < 4; ++q) {
         // (columns past N: no weights and no bias, so 0, which counts for no scale and is not stored)
-        const Bias16 bias = scalar_bias(g, nw + 32 * j + 16 * h);
+        auto word = [&](int w) {                          // of columns 32j + 8q + 4lh + 2w, + 1
+          const uint32_t lo = __builtin_amdgcn_readlane((int)bias, 16 * j + 4 * q + w), hi = __builtin_amdgcn_readlane((int)bias, 16 * j + 4 * q + 2 + w);
+          return lh ? hi : lo;
+        };
+        const uint32_t b[2] = {word(0), word(1)};
+        float v[4] = {acc[i][j][4 * q] + unpack_lo(b[0]), acc[i][j][4 * q + 1] + unpack_hi(b[0]),
+                      acc[i][j][4 * q + 2] + unpack_lo(b[1]), acc[i][j][4 * q + 3] + unpack_hi(b[1])};
 #pragma unroll
-        for (int q2 = 0; q2 < 2; ++q2) {
-          const int q = 2 * h + q2;
-          const uint32_t b0 = lh ? bias.w[4 * q2 + 2] : bias.w[4 * q2], b1 = lh ? bias.w[4 * q2 + 3] : bias.w[4 * q2 + 1];
-          float v[4] = {acc[i][j][4 * q] + unpack_lo(b0), acc[i][j][4 * q + 1] + unpack_hi(b0),
-                        acc[i][j][4 * q + 2] + unpack_lo(b1), acc[i][j][4 * q + 3] + unpack_hi(b1)};
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            if (GELU) v[e] = gelu_tanh(v[e]);
-            if (QUANT) {
-              acc[i][j][4 * q + e] = v[e];
-              largest = fmaxf(largest, finite_size(v[e]));
-            }
-          }
-          if (!QUANT) {
-            const u32x2_t pk = {pack_bf16x2_hw(v[0], v[1]), pack_bf16x2_hw(v[2], v[3])};
-            *reinterpret_cast<u32x2_t*>(region + lr * 256 + (((4 * j + q) ^ (lr & 15)) * 16) + lh * 8) = pk;
+        for (int e = 0; e < 4; ++e) {
+          if (GELU) v[e] = gelu_tanh(v[e]);
+          if (QUANT) {
+            acc[i][j][4 * q + e] = v[e];
+            largest = fmaxf(largest, finite_size(v[e]));
           }
         }
+        if (!QUANT) {
+          const u32x2_t pk = {pack_bf16x2_hw(v[0], v[1]), pack_bf16x2_hw(v[2], v[3])};
+          *reinterpret_cast<u32x2_t*>(region + lr * 128 + (((4 * (j & 1) + q) ^ ((lr >> 1) & 7)) * 16) + lh * 8) = pk;
+        }
       }
+      if (!QUANT && (j & 1)) {
+        // 32 rows x 8 pieces of 8 columns: one 128-byte line per row
+#pragma unroll
+        for (int it = 0; it < 4; ++it) {
+          const int rl = it * 8 + (lane >> 3), piece = lane & 7, n = nw + 64 * (j >> 1) + piece * 8;
+          const u32x4_t v = *reinterpret_cast<const u32x4_t*>(region + rl * 128 + ((piece ^ ((rl >> 1) & 7)) * 16));
+          __builtin_amdgcn_raw_buffer_store_b128(v, rs, n < g.n ? (uint32_t)(wm0 + 32 * i + rl) * row_bytes + (uint32_t)n * 2u : 0xFFFFFFF0u, 0, 0);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+      }
+    }
     if (QUANT) {
       const uint32_t byte = fp8_scale_of(fmaxf(largest, __shfl_xor(largest, 32, 64)));
       const float inv = fp8_inverse_scale(byte);
@@ -135,14 +137,6 @@ __device__ __forceinline__ void store_tile(const GemmFp8Args& g, floatx16_t (&ac
         const u32x4_t v = *reinterpret_cast<const u32x4_t*>(region + rl * 128 + ((piece ^ ((rl >> 1) & 7)) * 16));
         __builtin_amdgcn_raw_buffer_store_b128(v, rs, n < g.n ? (uint32_t)(wm0 + 32 * i + rl) * row_bytes + (uint32_t)n : 0xFFFFFFF0u, 0, 0);
       }
-    } else {
-      // 32 rows x 16 pieces of 8 columns: two 128-byte lines per row
-#pragma unroll
-      for (int it = 0; it < 8; ++it) {
-        const int rl = it * 4 + (lane >> 4), piece = lane & 15, n = nw + piece * 8;
-        const u32x4_t v = *reinterpret_cast<const u32x4_t*>(region + rl * 256 + ((piece ^ (rl & 15)) * 16));
-        __builtin_amdgcn_raw_buffer_store_b128(v, rs, n < g.n ? (uint32_t)(wm0 + 32 * i + rl) * row_bytes + (uint32_t)n * 2u : 0xFFFFFFF0u, 0, 0);
-      }
     }
     __builtin_amdgcn_sched_barrier(0);
   }
@@ -156,13 +150,15 @@ __global__ __launch_bounds__(512) void gemm256_fp8_kernel(GemmFp8Args g, int til
     int index, m0, n0, part, begin, end;         // part: the chunk's place among the partial sums; -1: a whole tile
   };
   auto item_from = [&](int index) {              // the first one from `index` on that is a tile (some slots are empty)
+    int tiles = tiles_n, group = group_m, parts = sk.split;
+    forget_scalar(tiles); forget_scalar(group); forget_scalar(parts);      // (reciprocals are formed here, not held through the loop)
     for (; index < n_items; index += gridDim.x) {
       const bool cut = index >= sk.full_items && sk.split > 1;
-      const int r = index - sk.full_items, slot = cut ? sk.full_items + r / sk.split : index, chunk = cut ? r % sk.split : 0;
+      const int r = index - sk.full_items, slot = cut ? sk.full_items + r / parts : index, chunk = cut ? r % parts : 0;
       int m0, n0;
-      if (tile_origin(slot, 256, 256, tiles_m, tiles_n, per_xcd, group_m, m0, n0))
-        return Item{index, m0, n0, cut ? r : -1, cut ? chunk_begin(chunk, sk.split, n_stages) : 0,
-                    cut ? chunk_begin(chunk + 1, sk.split, n_stages) : n_stages};
+      if (tile_origin(slot, 256, 256, tiles_m, tiles, per_xcd, group, m0, n0))
+        return Item{index, m0, n0, cut ? r : -1, cut ? chunk_begin(chunk, parts, n_stages) : 0,
+                    cut ? chunk_begin(chunk + 1, parts, n_stages) : n_stages};
     }
     return Item{-1, 0, 0, -1, 0, 0};
   };
@@ -176,25 +172,22 @@ __global__ __launch_bounds__(512) void gemm256_fp8_kernel(GemmFp8Args g, int til
   const int wm0 = (wave & 3) * 64, wn0 = (wave >> 2) * 128;
   const int lr = lane & 31, lh = lane >> 5;
 
-  // ---- fills: per stage this wave brings blocks wave+8i (8 rows each) of A and of W, i = 0..3; lane l fetches, for row l/8
-  //      of the block, the chunk that belongs in slot l%8.  Chunks past K are asked for past the buffer and arrive as zero. ----
+  // ---- fills: per stage this wave brings blocks wave+8q (8 rows each) of A, q = 0..3, and of each half of W, q = 0, 1; lane l
+  //      fetches, for row l/8 of the block, the chunk that belongs in slot l%8.  Half `hh` of W: rows 64*hh .. +63 and
+  //      128 + 64*hh .. +63 of the tile.  Chunks past K are asked for past the buffer and arrive as zero. ----
   const uint32_t row_bytes = (uint32_t)g.k;
   const u32x4_t rsA = rsrc_words(g.a, (uint32_t)g.m * row_bytes);
   const u32x4_t rsB = rsrc_words(g.w, (uint32_t)g.n * row_bytes);
-  const int row = wave * 8 + (lane >> 3);
-  const uint32_t fill_chunk = (lane & 7) ^ ((row >> 1) & 7);            // (the same for rows 64 apart)
   uint32_t voffA, voffB;
   const uint32_t step64 = 64u * row_bytes;
-  const uint32_t fillA = lds0 + wave * 1024, fillB = lds0 + RING_B_OFF + wave * 1024;
-  const uint32_t past = fill_chunk * 16 >= (uint32_t)(g.k - (n_stages - 1) * BK) ? 0xFFFFFFF0u : 0u;
-  auto voff = [&](uint32_t base, int stage, int q) {
-    return (base + (uint32_t)q * step64) | (stage == n_stages - 1 ? past : 0u);
-  };
+  uint32_t fillA = lds0 + wave * 1024, fillB = lds0 + RING_B_OFF + wave * 1024;
+  const uint32_t past = (uint32_t)((lane & 7) ^ ((wave * 4 + (lane >> 4)) & 7)) * 16u >= (uint32_t)(g.k - (n_stages - 1) * BK) ? 0xFFFFFFF0u : 0u;
   auto fill_a = [&](int slot, int stage, int q) {
-    lds_fill(rsA, fillA + (uint32_t)slot * STAGE_BYTES + q * 8192, voff(voffA, stage, q), (uint32_t)stage * BK);
+    lds_fill(rsA, fillA + (uint32_t)slot * STAGE_BYTES + q * 8192, (voffA + (uint32_t)q * step64) | (stage == n_stages - 1 ? past : 0u), (uint32_t)stage * BK);
   };
-  auto fill_b = [&](int slot, int stage, int q) {
-    lds_fill(rsB, fillB + (uint32_t)slot * STAGE_BYTES + q * 8192, voff(voffB, stage, q), (uint32_t)stage * BK);
+  auto fill_b = [&](int slot, int hh, int stage, int q) {
+    lds_fill(rsB, fillB + (uint32_t)slot * STAGE_BYTES + hh * (STAGE_BYTES / 2) + q * 8192,
+             (voffB + (uint32_t)(2 * q + hh) * step64) | (stage == n_stages - 1 ? past : 0u), (uint32_t)stage * BK);
   };
 
   // ---- scale bytes: of rows wm0 + 32i + lr, and of the wave's columns ----
@@ -203,7 +196,7 @@ __global__ __launch_bounds__(512) void gemm256_fp8_kernel(GemmFp8Args g, int til
   uint32_t wordA[2][WORDS], wordW[WORDS], nextA[2][WORDS], nextW[WORDS];
   auto ask_scales = [&](int m0, int n0, int stage) {
     int l = lane;
-    asm volatile("" : "+v"(l));
+    forget(l);
     const uint32_t at = (uint32_t)(m0 + wm0 + (l & 31)) * (uint32_t)pitch;
 #pragma unroll
     for (int w = 0; w < WORDS; ++w) {
@@ -217,47 +210,46 @@ __global__ __launch_bounds__(512) void gemm256_fp8_kernel(GemmFp8Args g, int til
     for (int w = 0; w < WORDS; ++w) {
       wordA[0][w] = nextA[0][w]; wordA[1][w] = nextA[1][w];
       wordW[w] = nextW[w];
-      asm volatile("" : "+v"(wordA[0][w]), "+v"(wordA[1][w]));
+      forget(wordA[0][w]); forget(wordA[1][w]);
     }
   };
 
   // ---- fragment reads: row R, chunk c of a stage sits at R*128 + (c ^ ((R/2)%8))*16.  A fragment of 64 k is the four
   //      chunks 4s .. 4s+3, the even ones to lanes 0-31: both operands take k in this order ----
-  uint32_t first = (uint32_t)(lr * 128 + ((lh ^ ((lr >> 1) & 7)) * 16));        // chunk lh of row lr
-  const uint32_t baseA = lds0 + wm0 * 128, baseB = lds0 + RING_B_OFF + wn0 * 128;
-  auto frag = [&](uint32_t base, int slice, int slot, int i) {
+  uint32_t firstA = lds0 + (uint32_t)(lr * 128 + ((lh ^ ((lr >> 1) & 7)) * 16)), firstB = firstA;      // chunk lh of row lr
+  firstA += wm0 * 128;
+  firstB += RING_B_OFF + (wn0 / 2) * 128;
+  auto frag = [&](uint32_t from, int slice, uint32_t offset) {
     typedef const __attribute__((address_space(3))) u32x4_t* lds_t;
-    const uint32_t at = base + slot * STAGE_BYTES + i * 4096;
-    const u32x4_t lo = *(lds_t)(size_t)((first ^ (uint32_t)(64 * slice)) + at), hi = *(lds_t)(size_t)((first ^ (uint32_t)(64 * slice + 32)) + at);
+    const u32x4_t lo = *(lds_t)(size_t)((from ^ (uint32_t)(64 * slice)) + offset), hi = *(lds_t)(size_t)((from ^ (uint32_t)(64 * slice + 32)) + offset);
     return i32x8_t{(int)lo[0], (int)lo[1], (int)lo[2], (int)lo[3], (int)hi[0], (int)hi[1], (int)hi[2], (int)hi[3]};
   };
 
   floatx16_t acc[2][4];
-  i32x8_t fa[2][2], fb[4];
+  i32x8_t fa[2][2], fb[4];                 // A fragments [slice][32 rows]; W fragments of a half stage
   int scaleA[2], scaleW;
-  // MFMA x of a stage: W fragment x/2 (slice x/8), A fragment x%2
-  auto mma = [&](int x) {
-    const int i = x & 1, u = (x >> 1) & 7, j = u & 3;
-    acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(fb[u & 3], fa[u >> 2][i], acc[i][j], 0, 0, 0, scaleW, 0, scaleA[i]);
+  // Half `hh` of stage t: MFMA x = 0..7 has slice x/4, W fragment x/2 (columns 64*hh + 32*(x/2%2)), A fragment x%2; each runs
+  // four steps after its first fragment was asked for, the last four of a half after the next barrier.
+  auto mma = [&](int x, int h) {
+    const int sl = x >> 2, j = 2 * (h & 1) + ((x >> 1) & 1), i = x & 1;
+    acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(fb[x >> 1], fa[sl][i], acc[i][j], 0, 0, 0, scaleW, 0, scaleA[i]);
   };
-  bool after_stores = false;               // the last item's stores lie between this one's first fills and the rest
-  auto stage = [&](auto SLOT_A, auto SLOT_B, int t) {
-    constexpr int SA = decltype(SLOT_A)::value, SB = decltype(SLOT_B)::value;
-    // All but the four newest fills (A of stage t+1) have landed: A and W of stage t are in LDS, and every wave's reads of
-    // stage t-1 are complete: its slots are free.
-    if (SA == 0 && SB == 0 && after_stores) {
-      after_stores = false;
-      asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(4 + TILE_STORES<QUANT>) : "memory");
-    } else {
-      asm volatile("s_waitcnt vmcnt(4) lgkmcnt(0)\n\ts_barrier" ::: "memory");
-    }
+  auto half_stage = [&](auto H, int t) {         // H: of the twelve halves after which slots and registers come round again
+    constexpr int h = decltype(H)::value, SA = h / 2 % 3, SB = h / 2 % 2, hh = h % 2;
+    // All but the eight newest fills have landed: this half of W, and at the first half all of A; every wave's reads of
+    // the half before are complete: its slot of W (at the first half: A's slot of stage t-1 too) is free.
+    asm volatile("s_waitcnt vmcnt(8) lgkmcnt(0)\n\ts_barrier" ::: "memory");
     __builtin_amdgcn_sched_barrier(0);
+    // (what follows from these is formed here again and not held in registers through the loop)
+    forget(firstA); forget(firstB); forget(voffA); forget(voffB);
+    forget_scalar(fillA); forget_scalar(fillB);
 #pragma unroll
-    for (int y = 0; y < 16; ++y) {
-      // (past the last stage it is fetched once more into the idle slot: in bounds, never read)
-      if (y < 4) fill_b(SB ^ 1, min(t + 1, it.end - 1), y);
-      else if (y < 8) fill_a((SA + 2) % 3, min(t + 2, it.end - 1), y - 4);
-      if (y == 4) {
+    for (int y = 0; y < 8; ++y) {
+      // the half of W three halves on, half of A two stages on (past the last stage it is fetched once more into the idle
+      // slot: in bounds, never read)
+      if (y < 2) fill_b(hh == 0 ? SB ^ 1 : SB, hh ^ 1, min(t + 1 + hh, it.end - 1), y);
+      else if (y < 4) fill_a((SA + 2) % 3, min(t + 2, it.end - 1), 2 * hh + y - 2);
+      if (hh == 0 && y == 4) {
         // the stage's own scales: byte 0 of the words, which move down by one
 #pragma unroll
         for (int i = 0; i < 2; ++i) scaleA[i] = (int)wordA[i][0];
@@ -270,82 +262,80 @@ __global__ __launch_bounds__(512) void gemm256_fp8_kernel(GemmFp8Args g, int til
           wordW[w] = w + 1 < WORDS ? (wordW[w] >> 8 | wordW[w + 1] << 24) : wordW[w] >> 8;
         }
       }
-      const int s = y >> 3, u = y >> 1;
-      // (what follows from these is formed here again and not held in registers through the loop)
-      if ((y & 7) == 0) asm volatile("" : "+v"(first), "+v"(voffA), "+v"(voffB));
-      if ((y & 7) == 0) fa[s][0] = frag(baseA, s, SA, 0);
-      if ((y & 1) == 0) fb[u & 3] = frag(baseB, s, SB, u & 3);
-      if ((y & 7) == 1) fa[s][1] = frag(baseA, s, SA, 1);
-      mma(y < 4 ? y + 12 : y - 4);
+      if (hh == 0 && (y & 3) < 2) fa[y >> 2][y & 1] = frag(firstA, y >> 2, SA * STAGE_BYTES + (y & 1) * 4096);
+      if ((y & 1) == 0) fb[y >> 1] = frag(firstB, y >> 2, SB * STAGE_BYTES + hh * (STAGE_BYTES / 2) + ((y >> 1) & 1) * 4096);
+      if (y >= 4) mma(y - 4, h);
+      else if (h != 0 || t != it.begin) mma(y + 4, h + 11);
       __builtin_amdgcn_sched_barrier(0);
     }
+  };
+  auto stage = [&](auto S, int t) {
+    half_stage(std::integral_constant<int, 2 * decltype(S)::value>{}, t);
+    half_stage(std::integral_constant<int, 2 * decltype(S)::value + 1>{}, t);
   };
   // what an item's main loop needs first: A and W of its first stage, A of the second
   auto start_item = [&]() {
     int l = lane;
-    asm volatile("" : "+v"(l));
-    const int row = wave * 8 + (l >> 3);
-    const uint32_t at = (uint32_t)row * row_bytes + (uint32_t)((l & 7) ^ ((row >> 1) & 7)) * 16u;
+    forget(l);
+    const uint32_t at = (uint32_t)(wave * 8 + (l >> 3)) * row_bytes + (uint32_t)((l & 7) ^ ((wave * 4 + (l >> 4)) & 7)) * 16u;
     voffA = (uint32_t)it.m0 * row_bytes + at;
     voffB = (uint32_t)it.n0 * row_bytes + at;
+    const int second = min(it.begin + 1, it.end - 1);
 #pragma unroll
     for (int q = 0; q < 4; ++q) fill_a(0, it.begin, q);
 #pragma unroll
-    for (int q = 0; q < 4; ++q) fill_b(0, it.begin, q);
+    for (int q = 0; q < 2; ++q) fill_b(0, 0, it.begin, q);
+    // (the eight that the first barrier need not wait for, in the order in which later ones do)
 #pragma unroll
-    for (int q = 0; q < 4; ++q) fill_a(1, min(it.begin + 1, it.end - 1), q);
+    for (int q = 0; q < 2; ++q) fill_b(0, 1, it.begin, q);
+#pragma unroll
+    for (int q = 0; q < 2; ++q) fill_a(1, second, q);
+#pragma unroll
+    for (int q = 0; q < 2; ++q) fill_b(1, 0, second, q);
+#pragma unroll
+    for (int q = 2; q < 4; ++q) fill_a(1, second, q);
   };
-  using I0 = std::integral_constant<int, 0>;
-  using I1 = std::integral_constant<int, 1>;
-  using I2 = std::integral_constant<int, 2>;
   ask_scales(it.m0, it.n0, it.begin);
   start_item();
   take_scales();
   for (;;) {
-    const Item next = item_from(it.index + gridDim.x);
 #pragma unroll
     for (int i = 0; i < 2; ++i)
 #pragma unroll
       for (int j = 0; j < 4; ++j)
 #pragma unroll
         for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.f;
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      fa[0][0][e] = fa[0][1][e] = fa[1][0][e] = fa[1][1][e] = 0;
-#pragma unroll
-      for (int u = 0; u < 4; ++u) fb[u][e] = 0;
-    }
-    scaleA[0] = scaleA[1] = scaleW = (int)FP8_SCALE_ONE;
     for (int t0 = it.begin;;) {
       const int group_end = min(t0 + GROUP, it.end);
       if (group_end < it.end) ask_scales(it.m0, it.n0, group_end);
-      else if (next.index >= 0) ask_scales(next.m0, next.n0, next.begin);
       for (int t = t0; t < group_end; t += 6) {
-        stage(I0{}, I0{}, t);
-        if (t + 1 < group_end) stage(I1{}, I1{}, t + 1);
-        if (t + 2 < group_end) stage(I2{}, I0{}, t + 2);
-        if (t + 3 < group_end) stage(I0{}, I1{}, t + 3);
-        if (t + 4 < group_end) stage(I1{}, I0{}, t + 4);
-        if (t + 5 < group_end) stage(I2{}, I1{}, t + 5);
+        stage(std::integral_constant<int, 0>{}, t);
+        if (t + 1 < group_end) stage(std::integral_constant<int, 1>{}, t + 1);
+        if (t + 2 < group_end) stage(std::integral_constant<int, 2>{}, t + 2);
+        if (t + 3 < group_end) stage(std::integral_constant<int, 3>{}, t + 3);
+        if (t + 4 < group_end) stage(std::integral_constant<int, 4>{}, t + 4);
+        if (t + 5 < group_end) stage(std::integral_constant<int, 5>{}, t + 5);
       }
       t0 = group_end;
       if (t0 >= it.end) break;
       take_scales();
     }
+    uint32_t bias = load_bias(g, it.n0 + wn0, lane);
 #pragma unroll
-    for (int x = 12; x < 16; ++x) mma(x);
+    for (int x = 4; x < 8; ++x) mma(x, 1);
 
     // Every wave is done with the rings, and no fill is in flight.  The next item's first fills go out before this one's
     // result is stored: they arrive, and the stores drain, behind other work.
     asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
     const Item done = it;
-    it = next;
+    forget(bias);                          // (awaited before new fills go out)
+    it = item_from(it.index + gridDim.x);
     if (it.index >= 0) {
-      take_scales();
+      ask_scales(it.m0, it.n0, it.begin);
       start_item();
     }
     int l = lane;
-    asm volatile("" : "+v"(l));            // (addresses are formed here, not held in registers through the loop)
+    forget(l);                             // (addresses are formed here, not held in registers through the loop)
     if (done.part >= 0) {
       float* part = sk.ws + (size_t)done.part * 65536 + wave * 256 + l * 4;
 #pragma unroll
@@ -358,12 +348,12 @@ __global__ __launch_bounds__(512) void gemm256_fp8_kernel(GemmFp8Args g, int til
             *reinterpret_cast<floatx4_t*>(part + ((i * 4 + j) * 4 + q) * 2048) = v;
           }
     } else {
-      // staging lies in the slots that the next item fills after its first barrier: the third of A, the second of W
-      char* region = reinterpret_cast<char*>(smem) + (wave < 4 ? 2 * STAGE_BYTES : RING_B_OFF) + wave * STAGING;
-      store_tile<QUANT, GELU>(g, acc, done.m0, wm0, done.n0 + wn0, l, region);
+      // staging lies in the slot that the next item fills after its first barrier: the third of A
+      char* region = reinterpret_cast<char*>(smem) + 2 * STAGE_BYTES + wave * STAGING;
+      store_tile<QUANT, GELU>(g, acc, bias, done.m0, wm0, done.n0 + wn0, l, region);
     }
     if (it.index < 0) return;
-    after_stores = true;
+    take_scales();
   }
 }
 
@@ -391,7 +381,8 @@ __global__ __launch_bounds__(64) void gemm256_fp8_fixup_kernel(GemmFp8Args g, in
 #pragma unroll
       for (int e = 0; e < 4; ++e) acc[x >> 4][(x >> 2) & 3][4 * (x & 3) + e] += v[x][e];
   }
-  store_tile<QUANT, GELU>(g, acc, m0, (wave & 3) * 64, n0 + (wave >> 2) * 128, lane, reinterpret_cast<char*>(smem));
+  const int nw = n0 + (wave >> 2) * 128;
+  store_tile<QUANT, GELU>(g, acc, load_bias(g, nw, lane), m0, (wave & 3) * 64, nw, lane, reinterpret_cast<char*>(smem));
 }
 
 template <bool QUANT, bool GELU>
@@ -580,7 +571,7 @@ __global__ __launch_bounds__(512) void gemm_fp8_halfk_kernel(GemmFp8Args g, int 
     // t-1 are complete, so its slot can be filled again
     asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"((RING - 2) * NF) : "memory");
     __builtin_amdgcn_sched_barrier(0);
-    asm volatile("" : "+v"(first));
+    forget(first);
     const uint32_t so = (uint32_t)slot * STAGE;
     const int refill = slot == 0 ? RING - 1 : slot - 1;
 #pragma unroll
@@ -622,7 +613,7 @@ __global__ __launch_bounds__(512) void gemm_fp8_halfk_kernel(GemmFp8Args g, int 
 #pragma unroll
       for (int i = 0; i < MB; ++i) {
         wordA[i][w] = nextA[i][w];
-        asm volatile("" : "+v"(wordA[i][w]));
+        forget(wordA[i][w]);
       }
 #pragma unroll
       for (int j = 0; j < NW; ++j) wordW[j][w] = nextW[j][w];
