@@ -36,16 +36,62 @@ constexpr int GEMM256_LDS = 5 * STAGE_BYTES;
 constexpr int GROUP = 12;                          // stages whose scale bytes are held: a multiple of 6 (ring slots) and 4
 constexpr int WORDS = GROUP / 4;
 
+// Division by a number that the host knows: exact while the dividend times the divisor stays below 2^32 (quick; the plain
+// division of a uniform value takes some 40 dependent instructions, 0.2 us, and there are three to a tile)
+struct Divisor {
+  uint32_t d = 1, mul = 0;             // mul 0: too large for that
+};
+inline Divisor divisor(uint32_t d, uint64_t most) {
+  return {d, (uint64_t)d * most < ((uint64_t)1 << 32) && d > 1 ? (uint32_t)((((uint64_t)1 << 32) + d - 1) / d) : 0u};
+}
+__device__ __forceinline__ uint32_t divide(uint32_t x, const Divisor& by) {
+  if (by.d == 1) return x;
+  return by.mul != 0 ? __umulhi(x, by.mul) : x / by.d;
+}
+
+// The tiles of a problem: slots are dealt so that each XCD owns a contiguous range of tiles, walked in groups of group_m row
+// tiles; some slots that pad the range to a multiple of 8 are empty.
+struct Grid {
+  int32_t tiles_m, tiles_n, per_xcd, group_m;
+  Divisor group, rows, last_rows;      // tiles of a group; row tiles of a group, of the last one
+};
+Grid make_grid(const GemmFp8Args& g, int bm, int bn) {
+  Grid t;
+  t.tiles_m = (g.m + bm - 1) / bm;
+  t.tiles_n = (g.n + bn - 1) / bn;
+  t.per_xcd = (t.tiles_m * t.tiles_n + 7) / 8;
+  // (operand panels of a long-k problem are several MB each, and a problem with few row tiles gives each XCD few groups)
+  t.group_m = (g.k >= 8192 || t.tiles_m <= 24) ? 4 : 8;
+  const uint64_t most = (uint64_t)t.per_xcd * 8;
+  t.group = divisor((uint32_t)(t.group_m * t.tiles_n), most);
+  t.rows = divisor((uint32_t)t.group_m, most);
+  t.last_rows = divisor((uint32_t)((t.tiles_m - 1) % t.group_m + 1), most);
+  return t;
+}
+// slot -> origin of its bm x bn tile; false for an empty one
+__device__ __forceinline__ bool origin(const Grid& t, int slot, int bm, int bn, int& m0, int& n0) {
+  const uint32_t p = (uint32_t)((slot % 8) * t.per_xcd + slot / 8);
+  if (p >= (uint32_t)(t.tiles_m * t.tiles_n)) return false;
+  const uint32_t group = divide(p, t.group), first_m = group * t.group_m;
+  const uint32_t in_group = p - group * t.group.d;
+  const bool last = first_m + t.group_m > (uint32_t)t.tiles_m;
+  const uint32_t rows = last ? t.last_rows.d : t.rows.d, column = last ? divide(in_group, t.last_rows) : divide(in_group, t.rows);
+  m0 = (int)(first_m + in_group - column * rows) * bm;
+  n0 = (int)column * bn;
+  return true;
+}
+
 // Tile slots 0 .. full_items-1 are whole work items; every later slot is cut into `split` chunks along k whose fp32 sums
 // go to a workspace (256 KB a chunk, in accumulator order) and are added up by the fix-up kernel.
 struct Split {
   int32_t full_items, split;
   float* ws;
+  Divisor by;                          // by split
 };
 
 // chunks begin on whole scale words
-__device__ __forceinline__ int chunk_begin(int chunk, int n_chunks, int n_stages) {
-  return chunk == n_chunks ? n_stages : chunk * n_stages / n_chunks / 4 * 4;
+__device__ __forceinline__ int chunk_begin(int chunk, int n_chunks, const Divisor& by, int n_stages) {
+  return chunk == n_chunks ? n_stages : (int)divide((uint32_t)(chunk * n_stages), by) / 4 * 4;
 }
 
 // Scale words of a weight's block of rows are the same for a whole wave: scalar loads (word clamped to the row's last)
@@ -57,16 +103,37 @@ __device__ __forceinline__ uint32_t weight_scale_word(const GemmFp8Args& g, int 
 }
 
 // Bias of a wave's 128 columns, two a lane; past the end of the buffer (columns past N, or no bias) zeros
-__device__ __forceinline__ uint32_t load_bias(const GemmFp8Args& g, int nw, int lane) {
-  const __amdgpu_buffer_rsrc_t rs = __builtin_amdgcn_make_buffer_rsrc(const_cast<bf16_t*>(g.bias), 0, g.bias != nullptr ? (uint32_t)g.n * 2u : 0u, 0x00020000);
+__device__ __forceinline__ uint32_t load_bias(const GemmFp8Args& g, int nw, int lane, bool none) {
+  const __amdgpu_buffer_rsrc_t rs =
+      __builtin_amdgcn_make_buffer_rsrc(const_cast<bf16_t*>(g.bias), 0, g.bias != nullptr && !none ? (uint32_t)g.n * 2u : 0u, 0x00020000);
   return __builtin_amdgcn_raw_buffer_load_b32(rs, (uint32_t)(nw + 2 * lane) * 2u, 0, 0);
+}
+
+// The sums begin with it: acc[i][j][4q+e] belongs to column nw + 32j + 8q + 4lh + e
+__device__ __forceinline__ void begin_with(uint32_t bias, int lane, floatx16_t (&acc)[2][4]) {
+  const bool high = lane >= 32;
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      auto word = [&](int w) {
+        const uint32_t lo = __builtin_amdgcn_readlane((int)bias, 16 * j + 4 * q + w), hi = __builtin_amdgcn_readlane((int)bias, 16 * j + 4 * q + 2 + w);
+        return high ? hi : lo;
+      };
+      const uint32_t a = word(0), b = word(1);
+      const float v[4] = {unpack_lo(a), unpack_hi(a), unpack_lo(b), unpack_hi(b)};
+#pragma unroll
+      for (int e = 0; e < 4; ++e) acc[0][j][4 * q + e] = acc[1][j][4 * q + e] = v[e];
+    }
+    __builtin_amdgcn_sched_barrier(0);
+  }
 }
 
 // A wave's 64 x 128 sums, acc[i][j][4q+e] = C[m0 + wm0 + 32i + lr][nw + 32j + 8q + 4lh + e], to the result, staged in two
 // quarters (8-bit results: halves) through 4 KB of this wave's LDS.  What lies outside the matrix is sent past the end of the buffer.
 constexpr int STAGING = 4096;
 template <bool QUANT, bool GELU>
-__device__ __forceinline__ void store_tile(const GemmFp8Args& g, floatx16_t (&acc)[2][4], uint32_t bias, int m0, int wm0, int nw,
+__device__ __forceinline__ void store_tile(const GemmFp8Args& g, floatx16_t (&acc)[2][4], int m0, int wm0, int nw,
                                            int lane, char* region) {
   const int out_pitch = fp8_scale_pitch(g.n), block = nw >> 7, blocks = (g.n + 127) >> 7;
   const uint32_t row_bytes = (uint32_t)g.n * (QUANT ? 1u : 2u);
@@ -75,7 +142,7 @@ __device__ __forceinline__ void store_tile(const GemmFp8Args& g, floatx16_t (&ac
   const __amdgpu_buffer_rsrc_t rs = __builtin_amdgcn_make_buffer_rsrc(base, 0, rows * row_bytes, 0x00020000);
 #pragma unroll
   for (int i = 0; i < 2; ++i) {
-    forget(bias); forget(lane);            // (what follows from these is formed again, not held from the first half)
+    forget(lane);                          // (what follows from it is formed again, not held from the first half)
     const int lr = lane & 31, lh = lane >> 5;
     float largest = 0.f;
 #pragma unroll
@@ -83,13 +150,7 @@ __device__ __forceinline__ void store_tile(const GemmFp8Args& g, floatx16_t (&ac
 #pragma unroll
       for (int q = 0; q < 4; ++q) {
         // (columns past N: no weights and no bias, so 0, which counts for no scale and is not stored)
-        auto word = [&](int w) {                          // of columns 32j + 8q + 4lh + 2w, + 1
-          const uint32_t lo = __builtin_amdgcn_readlane((int)bias, 16 * j + 4 * q + w), hi = __builtin_amdgcn_readlane((int)bias, 16 * j + 4 * q + 2 + w);
-          return lh ? hi : lo;
-        };
-        const uint32_t b[2] = {word(0), word(1)};
-        float v[4] = {acc[i][j][4 * q] + unpack_lo(b[0]), acc[i][j][4 * q + 1] + unpack_hi(b[0]),
-                      acc[i][j][4 * q + 2] + unpack_lo(b[1]), acc[i][j][4 * q + 3] + unpack_hi(b[1])};
+        float v[4] = {acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]};
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
           if (GELU) v[e] = gelu_tanh(v[e]);
@@ -142,23 +203,38 @@ __device__ __forceinline__ void store_tile(const GemmFp8Args& g, floatx16_t (&ac
   }
 }
 
+struct Args256 {
+  GemmFp8Args g;
+  Grid grid;
+  Split sk;
+};
+// The kernel's arguments, read again where they are used: between tiles, so that no register holds them in the main loop
+__device__ __forceinline__ const Args256& args_again() {
+  auto p = __builtin_amdgcn_kernarg_segment_ptr();
+  forget_scalar(p);
+  return *(const Args256*)p;
+}
+
 template <bool QUANT, bool GELU>
-__global__ __launch_bounds__(512) void gemm256_fp8_kernel(GemmFp8Args g, int tiles_m, int tiles_n, int per_xcd, int group_m, Split sk) {
+__global__ __launch_bounds__(512) void gemm256_fp8_kernel(Args256 args) {
+  const GemmFp8Args& g = args.g;
   // ---- the work items of this workgroup: blockIdx.x, then every gridDim.x-th; a whole tile or a chunk of one ----
-  const int slots = 8 * per_xcd, n_items = sk.full_items + (slots - sk.full_items) * sk.split, n_stages = (g.k + BK - 1) / BK;
+  const int n_stages = (g.k + BK - 1) / BK;
   struct Item {
     int index, m0, n0, part, begin, end;         // part: the chunk's place among the partial sums; -1: a whole tile
   };
   auto item_from = [&](int index) {              // the first one from `index` on that is a tile (some slots are empty)
-    int tiles = tiles_n, group = group_m, parts = sk.split;
-    forget_scalar(tiles); forget_scalar(group); forget_scalar(parts);      // (reciprocals are formed here, not held through the loop)
+    const Args256 now = args_again();
+    const Grid& grid = now.grid;
+    const Split& sk = now.sk;
+    const int n_items = sk.full_items + (8 * grid.per_xcd - sk.full_items) * sk.split;
     for (; index < n_items; index += gridDim.x) {
       const bool cut = index >= sk.full_items && sk.split > 1;
-      const int r = index - sk.full_items, slot = cut ? sk.full_items + r / parts : index, chunk = cut ? r % parts : 0;
+      const int r = index - sk.full_items, tile = cut ? (int)divide((uint32_t)r, sk.by) : 0, chunk = r - tile * sk.split;
       int m0, n0;
-      if (tile_origin(slot, 256, 256, tiles_m, tiles, per_xcd, group, m0, n0))
-        return Item{index, m0, n0, cut ? r : -1, cut ? chunk_begin(chunk, parts, n_stages) : 0,
-                    cut ? chunk_begin(chunk + 1, parts, n_stages) : n_stages};
+      if (origin(grid, cut ? sk.full_items + tile : index, 256, 256, m0, n0))
+        return Item{index, m0, n0, cut ? r : -1, cut ? chunk_begin(chunk, sk.split, sk.by, n_stages) : 0,
+                    cut ? chunk_begin(chunk + 1, sk.split, sk.by, n_stages) : n_stages};
     }
     return Item{-1, 0, 0, -1, 0, 0};
   };
@@ -295,16 +371,12 @@ __global__ __launch_bounds__(512) void gemm256_fp8_kernel(GemmFp8Args g, int til
 #pragma unroll
     for (int q = 2; q < 4; ++q) fill_a(1, second, q);
   };
+  uint32_t bias = load_bias(g, it.n0 + wn0, lane, it.part >= 0);           // (cut tiles: added by the fix-up kernel)
   ask_scales(it.m0, it.n0, it.begin);
   start_item();
   take_scales();
   for (;;) {
-#pragma unroll
-    for (int i = 0; i < 2; ++i)
-#pragma unroll
-      for (int j = 0; j < 4; ++j)
-#pragma unroll
-        for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.f;
+    begin_with(bias, lane, acc);
     for (int t0 = it.begin;;) {
       const int group_end = min(t0 + GROUP, it.end);
       if (group_end < it.end) ask_scales(it.m0, it.n0, group_end);
@@ -320,7 +392,6 @@ __global__ __launch_bounds__(512) void gemm256_fp8_kernel(GemmFp8Args g, int til
       if (t0 >= it.end) break;
       take_scales();
     }
-    uint32_t bias = load_bias(g, it.n0 + wn0, lane);
 #pragma unroll
     for (int x = 4; x < 8; ++x) mma(x, 1);
 
@@ -328,16 +399,16 @@ __global__ __launch_bounds__(512) void gemm256_fp8_kernel(GemmFp8Args g, int til
     // result is stored: they arrive, and the stores drain, behind other work.
     asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
     const Item done = it;
-    forget(bias);                          // (awaited before new fills go out)
     it = item_from(it.index + gridDim.x);
     if (it.index >= 0) {
+      bias = load_bias(args_again().g, it.n0 + wn0, lane, it.part >= 0);
       ask_scales(it.m0, it.n0, it.begin);
       start_item();
     }
     int l = lane;
     forget(l);                             // (addresses are formed here, not held in registers through the loop)
     if (done.part >= 0) {
-      float* part = sk.ws + (size_t)done.part * 65536 + wave * 256 + l * 4;
+      float* part = args_again().sk.ws + (size_t)done.part * 65536 + wave * 256 + l * 4;
 #pragma unroll
       for (int i = 0; i < 2; ++i)
 #pragma unroll
@@ -350,7 +421,7 @@ __global__ __launch_bounds__(512) void gemm256_fp8_kernel(GemmFp8Args g, int til
     } else {
       // staging lies in the slot that the next item fills after its first barrier: the third of A
       char* region = reinterpret_cast<char*>(smem) + 2 * STAGE_BYTES + wave * STAGING;
-      store_tile<QUANT, GELU>(g, acc, bias, done.m0, wm0, done.n0 + wn0, l, region);
+      store_tile<QUANT, GELU>(args_again().g, acc, done.m0, wm0, done.n0 + wn0, l, region);
     }
     if (it.index < 0) return;
     take_scales();
@@ -359,18 +430,14 @@ __global__ __launch_bounds__(512) void gemm256_fp8_kernel(GemmFp8Args g, int til
 
 // Adds up the chunks of the cut tiles and stores the result: a one-wave workgroup to each 64 x 128 part of a tile.
 template <bool QUANT, bool GELU>
-__global__ __launch_bounds__(64) void gemm256_fp8_fixup_kernel(GemmFp8Args g, int tiles_m, int tiles_n, int per_xcd, int group_m, Split sk) {
+__global__ __launch_bounds__(64) void gemm256_fp8_fixup_kernel(GemmFp8Args g, Grid grid, Split sk) {
   const int tile = blockIdx.x >> 3, wave = blockIdx.x & 7, lane = threadIdx.x;
   int m0, n0;
-  if (!tile_origin(sk.full_items + tile, 256, 256, tiles_m, tiles_n, per_xcd, group_m, m0, n0)) return;
+  if (!origin(grid, sk.full_items + tile, 256, 256, m0, n0)) return;
   extern __shared__ u32x4_t smem[];
   floatx16_t acc[2][4];
-#pragma unroll
-  for (int i = 0; i < 2; ++i)
-#pragma unroll
-    for (int j = 0; j < 4; ++j)
-#pragma unroll
-      for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.f;
+  const int nw = n0 + (wave >> 2) * 128;
+  begin_with(load_bias(g, nw, lane, false), lane, acc);
   const float* part = sk.ws + (size_t)tile * sk.split * 65536 + (wave * 64 + lane) * 4;
   for (int c = 0; c < sk.split; ++c, part += 65536) {
     floatx4_t v[32];
@@ -381,8 +448,7 @@ __global__ __launch_bounds__(64) void gemm256_fp8_fixup_kernel(GemmFp8Args g, in
 #pragma unroll
       for (int e = 0; e < 4; ++e) acc[x >> 4][(x >> 2) & 3][4 * (x & 3) + e] += v[x][e];
   }
-  const int nw = n0 + (wave >> 2) * 128;
-  store_tile<QUANT, GELU>(g, acc, load_bias(g, nw, lane), m0, (wave & 3) * 64, nw, lane, reinterpret_cast<char*>(smem));
+  store_tile<QUANT, GELU>(g, acc, m0, (wave & 3) * 64, nw, lane, reinterpret_cast<char*>(smem));
 }
 
 template <bool QUANT, bool GELU>
@@ -391,15 +457,14 @@ hipError_t launch_gemm256_fp8(const GemmFp8Args& g, int split, hipStream_t st) {
   auto kern = gemm256_fp8_kernel<QUANT, GELU>;
   hipError_t e = allow_dynamic_lds(reinterpret_cast<const void*>(kern), GEMM256_LDS, lds_allowed);
   if (e != hipSuccess) return e;
-  const int tiles_m = (g.m + 255) / 256, tiles_n = (g.n + 255) / 256;
-  const int per_xcd = (tiles_m * tiles_n + 7) / 8, slots = per_xcd * 8;
-  const int group_m = (g.k >= 8192 || tiles_m <= 24) ? 4 : 8;
-  const Split sk = {split > 1 ? slots / 256 * 256 : slots, split, g.scratch};
+  const Grid grid = make_grid(g, 256, 256);
+  const int slots = grid.per_xcd * 8;
+  const Split sk = {split > 1 ? slots / 256 * 256 : slots, split, g.scratch, divisor((uint32_t)split, 1u << 28)};
   const int cut = slots - sk.full_items;
   if ((size_t)cut * sk.split * 262144 > (cut > 0 ? g.scratch_bytes : 0)) return hipErrorInvalidValue;
-  hipLaunchKernelGGL(kern, dim3(std::min(sk.full_items + cut * sk.split, 256)), dim3(512), GEMM256_LDS, st, g, tiles_m, tiles_n, per_xcd, group_m, sk);
+  hipLaunchKernelGGL(kern, dim3(std::min(sk.full_items + cut * sk.split, 256)), dim3(512), GEMM256_LDS, st, Args256{g, grid, sk});
   if (cut > 0)
-    hipLaunchKernelGGL((gemm256_fp8_fixup_kernel<QUANT, GELU>), dim3(cut * 8), dim3(64), STAGING, st, g, tiles_m, tiles_n, per_xcd, group_m, sk);
+    hipLaunchKernelGGL((gemm256_fp8_fixup_kernel<QUANT, GELU>), dim3(cut * 8), dim3(64), STAGING, st, g, grid, sk);
   return hipGetLastError();
 }
 
@@ -460,12 +525,14 @@ __device__ __forceinline__ void stream_tile(const GemmFp8Args& g, int m0, int n0
 struct Cut {
   int32_t full_items, tiles, chunks;
   float* parts;
+  Divisor by_tiles, by_chunks;
 };
 struct CutItem { int slot, chunk, n_chunks; };
 __device__ __forceinline__ CutItem cut_item(const Cut& cut) {
   const int r = (int)blockIdx.x - cut.full_items;
   if (r < 0) return {(int)blockIdx.x, 0, 1};
-  return {cut.full_items + r % cut.tiles, r / cut.tiles, cut.chunks};
+  const int chunk = (int)divide((uint32_t)r, cut.by_tiles);
+  return {cut.full_items + r - chunk * cut.tiles, chunk, cut.chunks};
 }
 
 // BM x BN tile, eight waves: 2 x 2 sub-tiles, each computed by two waves that take one half of every stage of 128 k.  The
@@ -482,7 +549,7 @@ struct HalfK {
 };
 
 template <int BM, int BN, bool QUANT, bool GELU>
-__global__ __launch_bounds__(512) void gemm_fp8_halfk_kernel(GemmFp8Args g, int tiles_m, int tiles_n, int per_xcd, int group_m, Cut cut) {
+__global__ __launch_bounds__(512) void gemm_fp8_halfk_kernel(GemmFp8Args g, Grid grid, Cut cut) {
   using C = HalfK<BM, BN>;
   constexpr int MB = BM / 64, NB = BN / 64;            // 32 x 32 blocks of a wave's BM/2 x BN/2 sub-tile
   constexpr int NF = (BM + BN) / 64;                   // 1 KB fills of a wave per stage
@@ -491,7 +558,7 @@ __global__ __launch_bounds__(512) void gemm_fp8_halfk_kernel(GemmFp8Args g, int 
   static_assert(BM % 64 == 0 && BN % 64 == 0 && RING >= 3 && NB >= 2, "tile shape");
   const CutItem it = cut_item(cut);
   int m0, n0;
-  if (!tile_origin(it.slot, BM, BN, tiles_m, tiles_n, per_xcd, group_m, m0, n0)) return;
+  if (!origin(grid, it.slot, BM, BN, m0, n0)) return;
 
   extern __shared__ u32x4_t smem[];
   const uint32_t lds0 = (uint32_t)(size_t)(__attribute__((address_space(3))) void*)smem;
@@ -509,7 +576,8 @@ __global__ __launch_bounds__(512) void gemm_fp8_halfk_kernel(GemmFp8Args g, int 
   const uint32_t voffA = (uint32_t)(m0 + row) * row_bytes + fill_chunk * 16, voffB = (uint32_t)(n0 + row) * row_bytes + fill_chunk * 16;
   const uint32_t step64 = 64u * row_bytes;
   const int n_stages = (g.k + BK - 1) / BK;
-  const int stage_begin = chunk_begin(it.chunk, it.n_chunks, n_stages), stage_end = chunk_begin(it.chunk + 1, it.n_chunks, n_stages);
+  const int stage_begin = it.n_chunks == 1 ? 0 : chunk_begin(it.chunk, it.n_chunks, cut.by_chunks, n_stages);
+  const int stage_end = it.n_chunks == 1 ? n_stages : chunk_begin(it.chunk + 1, it.n_chunks, cut.by_chunks, n_stages);
   const uint32_t past = fill_chunk * 16 >= (uint32_t)(g.k - (n_stages - 1) * BK) ? 0xFFFFFFF0u : 0u;
   auto fill = [&](int slot, int want, int i) {
     const int stage = min(want, stage_end - 1);        // (past the end: the last stage again, unread)
@@ -671,11 +739,11 @@ __global__ __launch_bounds__(512) void gemm_fp8_halfk_kernel(GemmFp8Args g, int 
 
 // Adds up the chunks of cut tiles and stores the result; 16 rows of a tile to a workgroup.
 template <int BM, int BN, bool QUANT, bool GELU>
-__global__ __launch_bounds__(256) void gemm_fp8_fixup_kernel(GemmFp8Args g, int tiles_m, int tiles_n, int per_xcd, int group_m, Cut cut) {
+__global__ __launch_bounds__(256) void gemm_fp8_fixup_kernel(GemmFp8Args g, Grid grid, Cut cut) {
   constexpr int ROWS = 16;
   const int tile = blockIdx.x / (BM / ROWS), r0 = blockIdx.x % (BM / ROWS) * ROWS;
   int m0, n0;
-  if (!tile_origin(cut.full_items + tile, BM, BN, tiles_m, tiles_n, per_xcd, group_m, m0, n0)) return;
+  if (!origin(grid, cut.full_items + tile, BM, BN, m0, n0)) return;
   const float* part = cut.parts + (size_t)tile * cut.chunks * (BM * BN) + r0 * BN;
   stream_tile<QUANT, GELU, ROWS, BN, 256>(g, m0 + r0, n0, threadIdx.x, [&](int ml, int nl, float* v) {
     const float* p = part + ml * BN + nl;
@@ -832,15 +900,13 @@ hipError_t launch_halfk(const GemmFp8Args& g, int chunks, hipStream_t st) {
   auto kern = gemm_fp8_halfk_kernel<BM, BN, QUANT, GELU>;
   hipError_t e = allow_dynamic_lds(reinterpret_cast<const void*>(kern), HalfK<BM, BN>::LDS, lds_allowed);
   if (e != hipSuccess) return e;
-  const int tiles_m = (g.m + BM - 1) / BM, tiles_n = (g.n + BN - 1) / BN;
-  const int per_xcd = (tiles_m * tiles_n + 7) / 8, slots = per_xcd * 8;
-  const int group_m = (g.k >= 8192 || tiles_m <= 24) ? 4 : 8;
-  const int full = chunks > 1 ? slots / 256 * 256 : slots;
-  const Cut cut = {full, slots - full, chunks, g.scratch};
+  const Grid grid = make_grid(g, BM, BN);
+  const int slots = grid.per_xcd * 8, full = chunks > 1 ? slots / 256 * 256 : slots;
+  const Cut cut = {full, slots - full, chunks, g.scratch, divisor((uint32_t)(slots - full), 4096), divisor((uint32_t)chunks, 1u << 28)};
   if ((size_t)cut.tiles * chunks * (BM * BN * 4) > (cut.tiles > 0 ? g.scratch_bytes : 0)) return hipErrorInvalidValue;
-  hipLaunchKernelGGL(kern, dim3(full + (slots - full) * chunks), dim3(512), (HalfK<BM, BN>::LDS), st, g, tiles_m, tiles_n, per_xcd, group_m, cut);
+  hipLaunchKernelGGL(kern, dim3(full + (slots - full) * chunks), dim3(512), (HalfK<BM, BN>::LDS), st, g, grid, cut);
   if (slots > full)
-    hipLaunchKernelGGL((gemm_fp8_fixup_kernel<BM, BN, QUANT, GELU>), dim3((slots - full) * (BM / 16)), dim3(256), 0, st, g, tiles_m, tiles_n, per_xcd, group_m, cut);
+    hipLaunchKernelGGL((gemm_fp8_fixup_kernel<BM, BN, QUANT, GELU>), dim3((slots - full) * (BM / 16)), dim3(256), 0, st, g, grid, cut);
   return hipGetLastError();
 }
 

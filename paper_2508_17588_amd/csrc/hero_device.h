@@ -101,21 +101,6 @@ __device__ __forceinline__ void lds_fill(u32x4_t rsrc, uint32_t lds_addr, uint32
                :: "s"(lds_addr), "v"(voffset), "s"(rsrc) : "memory");
 }
 
-// tile slot -> origin of its bm x bn tile (each XCD owns a contiguous range of tiles, walked in groups of
-// group_m row tiles); false for the empty slots that pad the range to a multiple of 8
-__device__ __forceinline__ bool tile_origin(int slot, int bm, int bn, int tiles_m, int tiles_n, int per_xcd,
-                                            int group_m, int& m0, int& n0) {
-  const int p = (slot % 8) * per_xcd + slot / 8;
-  if (p >= tiles_m * tiles_n) return false;
-  const int group = p / (group_m * tiles_n);
-  const int first_m = group * group_m;
-  const int gsize = min(tiles_m - first_m, group_m);
-  const int in_group = p - group * group_m * tiles_n;
-  m0 = (first_m + in_group % gsize) * bm;
-  n0 = (in_group / gsize) * bn;
-  return true;
-}
-
 __device__ __forceinline__ float gelu_tanh(float x) {
   // x/2 (1 + tanh u) = x / (1 + exp(-2u)),  u = sqrt(2/pi) (x + 0.044715 x^3);
   // -2u log2(e) = x (C1 + C2 x^2) with the constants folded: five plain operations and two
