@@ -33,12 +33,15 @@ __device__ __forceinline__ uint32_t fp8_scale_of(float largest) {
   const int byte = (int)(u >> 23) - 8 + ((u & 0x7FFFFFu) > 0x600000u ? 1 : 0);
   return u == 0 ? FP8_SCALE_ONE : (uint32_t)max(byte, 0);
 }
-// 1 / scale; bytes that fp8_scale_of gives are at most 247
-__device__ __forceinline__ float fp8_inverse_scale(uint32_t byte) { return __uint_as_float((254u - byte) << 23); }
-
-// four values, already over their scale, as e4m3, round to nearest even (beyond 464 and NaN: NaN)
-__device__ __forceinline__ uint32_t pack_fp8x4(float a, float b, float c, float d) {
-  return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(c, d, __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false), true);
+// four values over their scale as e4m3, round to nearest even (beyond 464 and NaN: NaN).  The conversion takes the scale's
+// exponent, all bytes from 0 (2^-127) on among them, and divides by it without rounding.
+__device__ __forceinline__ uint32_t pack_fp8x4(float a, float b, float c, float d, uint32_t scale_byte) {
+  typedef short i16x2_t __attribute__((ext_vector_type(2)));
+  const float scale = __uint_as_float(scale_byte << 23);
+  i16x2_t out = {0, 0};
+  out = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(out, a, b, scale, false);
+  out = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(out, c, d, scale, true);
+  return __builtin_bit_cast(uint32_t, out);
 }
 
 // A value the compiler knows nothing of from here on: what follows from it is formed again where it is used, and not kept in

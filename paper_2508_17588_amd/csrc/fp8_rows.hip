@@ -19,10 +19,9 @@ __device__ __forceinline__ void store_piece(const float* v, uint8_t* q, bool in_
 #pragma unroll
   for (int e = 0; e < 8; ++e) largest = fmaxf(largest, finite_size(v[e]));
   const uint32_t byte = fp8_scale_of(max_of_16_lanes(largest));
-  const float inv = fp8_inverse_scale(byte);
   if (in_row) {
-    const u32x2_t out = {pack_fp8x4(v[0] * inv, v[1] * inv, v[2] * inv, v[3] * inv),
-                         pack_fp8x4(v[4] * inv, v[5] * inv, v[6] * inv, v[7] * inv)};
+    const u32x2_t out = {pack_fp8x4(v[0], v[1], v[2], v[3], byte),
+                         pack_fp8x4(v[4], v[5], v[6], v[7], byte)};
     *reinterpret_cast<u32x2_t*>(q) = out;
   }
   uint32_t word = 0;
@@ -134,13 +133,12 @@ __global__ __launch_bounds__(256) void quantize_blocks_kernel(const XT* __restri
   __syncthreads();
   largest = fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3]));
   const uint32_t byte = fp8_scale_of(largest);
-  const float inv = fp8_inverse_scale(byte);
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
     if (c >= columns || r0 + 16 * i >= n_rows) continue;
     const float* t = v[i];
-    const u32x2_t o = {pack_fp8x4(t[0] * inv, t[1] * inv, t[2] * inv, t[3] * inv),
-                       pack_fp8x4(t[4] * inv, t[5] * inv, t[6] * inv, t[7] * inv)};
+    const u32x2_t o = {pack_fp8x4(t[0], t[1], t[2], t[3], byte),
+                       pack_fp8x4(t[4], t[5], t[6], t[7], byte)};
     *reinterpret_cast<u32x2_t*>(out.q + (int64_t)(r0 + 16 * i) * columns + c) = o;
   }
   // the last block of a row of blocks also writes the bytes that fill the word

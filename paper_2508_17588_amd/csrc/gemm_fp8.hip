@@ -156,7 +156,7 @@ __device__ __forceinline__ void store_tile(const GemmFp8Args& g, floatx16_t (&ac
           if (GELU) v[e] = gelu_tanh(v[e]);
           if (QUANT) {
             acc[i][j][4 * q + e] = v[e];
-            largest = fmaxf(largest, finite_size(v[e]));
+            largest = fmaxf(largest, __builtin_fabsf(v[e]));       // (NaN does not count; infinities below)
           }
         }
         if (!QUANT) {
@@ -176,14 +176,20 @@ __device__ __forceinline__ void store_tile(const GemmFp8Args& g, floatx16_t (&ac
       }
     }
     if (QUANT) {
+      if (__any(largest == __builtin_inff())) {
+        largest = 0.f;
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+#pragma unroll
+          for (int e = 0; e < 16; ++e) largest = fmaxf(largest, finite_size(acc[i][j][e]));
+      }
       const uint32_t byte = fp8_scale_of(fmaxf(largest, __shfl_xor(largest, 32, 64)));
-      const float inv = fp8_inverse_scale(byte);
 #pragma unroll
       for (int j = 0; j < 4; ++j)
 #pragma unroll
         for (int q = 0; q < 4; ++q)
           *reinterpret_cast<uint32_t*>(region + lr * 128 + (((2 * j + (q >> 1)) ^ ((lr >> 1) & 7)) * 16) + (q & 1) * 8 + lh * 4) =
-              pack_fp8x4(acc[i][j][4 * q] * inv, acc[i][j][4 * q + 1] * inv, acc[i][j][4 * q + 2] * inv, acc[i][j][4 * q + 3] * inv);
+              pack_fp8x4(acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3], byte);
       const int m = m0 + wm0 + 32 * i + lr;
       if (lh == 0 && m < g.m && nw < g.n) {
         uint8_t* s = g.out.scales + (int64_t)m * out_pitch;
@@ -503,10 +509,9 @@ __device__ __forceinline__ void stream_tile(const GemmFp8Args& g, int m0, int n0
 #pragma unroll
       for (int e = 0; e < 8; ++e) largest = fmaxf(largest, n < g.n ? finite_size(v[e]) : 0.f);
       const uint32_t byte = fp8_scale_of(max_of_16_lanes(largest));
-      const float inv = fp8_inverse_scale(byte);
       if (m < g.m && n < g.n) {
-        const u32x2_t out = {pack_fp8x4(v[0] * inv, v[1] * inv, v[2] * inv, v[3] * inv),
-                             pack_fp8x4(v[4] * inv, v[5] * inv, v[6] * inv, v[7] * inv)};
+        const u32x2_t out = {pack_fp8x4(v[0], v[1], v[2], v[3], byte),
+                             pack_fp8x4(v[4], v[5], v[6], v[7], byte)};
         *reinterpret_cast<u32x2_t*>(g.out.q + (int64_t)m * g.n + n) = out;
       }
       if (m < g.m && nl == 0) {

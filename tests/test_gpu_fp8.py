@@ -281,6 +281,18 @@ def test_linear_special_values(m):
     run_linear((aq, sa2.view(torch.float8_e8m0fnu)), (wq, ws), bias, 0, True)
 
 
+@pytest.mark.parametrize("m,n,k", [(3, 272, 160), (200, 272, 160), (700, 1040, 2048), (40, 144, 4112)])
+def test_infinite_results_in_8_bits(m, n, k):
+    """An infinite result is a NaN element and does not count for its block's scale."""
+    say(f"infinite results {m} x {n} x {k}")
+    a, w, bias = operands(m, n, k)
+    bias[5], bias[140], bias[141] = INF, -INF, NAN
+    scratch = torch.empty(64 << 20, dtype=torch.uint8, device="cuda")
+    for act in (0, 1):
+        run_linear(a, w, bias, act, True, scratch=scratch)
+        run_linear(a, w, bias, act, False, scratch=scratch)
+
+
 def test_padding_bytes_of_scales_are_not_used():
     say("padding of the scales")
     m, n, k = 70, 144, 272
