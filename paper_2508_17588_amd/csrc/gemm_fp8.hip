@@ -458,14 +458,24 @@ __global__ __launch_bounds__(64) void gemm256_fp8_fixup_kernel(GemmFp8Args g, Gr
 }
 
 template <bool QUANT, bool GELU>
-hipError_t launch_gemm256_fp8(const GemmFp8Args& g, int split, hipStream_t st) {
+hipError_t launch_quarters(const GemmFp8Args& g, const Grid& grid, hipStream_t st);
+
+// quarters: the tiles of the last, partly filled round go to a second kernel, four workgroups to a tile
+template <bool QUANT, bool GELU>
+hipError_t launch_gemm256_fp8(const GemmFp8Args& g, int split, bool quarters, hipStream_t st) {
   static std::atomic<uint64_t> lds_allowed{0};
   auto kern = gemm256_fp8_kernel<QUANT, GELU>;
   hipError_t e = allow_dynamic_lds(reinterpret_cast<const void*>(kern), GEMM256_LDS, lds_allowed);
   if (e != hipSuccess) return e;
   const Grid grid = make_grid(g, 256, 256);
   const int slots = grid.per_xcd * 8;
-  const Split sk = {split > 1 ? slots / 256 * 256 : slots, split, g.scratch, divisor((uint32_t)split, 1u << 28)};
+  const int whole = slots / 256 * 256;
+  if (quarters) {
+    // (no item after the whole ones)
+    if (whole > 0) hipLaunchKernelGGL(kern, dim3(256), dim3(512), GEMM256_LDS, st, Args256{g, grid, Split{whole, 0, nullptr, Divisor()}});
+    return whole < slots ? launch_quarters<QUANT, GELU>(g, grid, st) : hipGetLastError();
+  }
+  const Split sk = {split > 1 ? whole : slots, split, g.scratch, divisor((uint32_t)split, 1u << 28)};
   const int cut = slots - sk.full_items;
   if ((size_t)cut * sk.split * 262144 > (cut > 0 ? g.scratch_bytes : 0)) return hipErrorInvalidValue;
   hipLaunchKernelGGL(kern, dim3(std::min(sk.full_items + cut * sk.split, 256)), dim3(512), GEMM256_LDS, st, Args256{g, grid, sk});
@@ -532,9 +542,11 @@ struct Cut {
   float* parts;
   Divisor by_tiles, by_chunks;
 };
+// QUARTERS: the tiles after full_items are 256 x 256, of which a "chunk" is a quarter of 128 x 128 with all of k.
 struct CutItem { int slot, chunk, n_chunks; };
+template <bool QUARTERS>
 __device__ __forceinline__ CutItem cut_item(const Cut& cut) {
-  const int r = (int)blockIdx.x - cut.full_items;
+  const int r = QUARTERS ? (int)blockIdx.x : (int)blockIdx.x - cut.full_items;      // (a kernel for quarters has nothing else)
   if (r < 0) return {(int)blockIdx.x, 0, 1};
   const int chunk = (int)divide((uint32_t)r, cut.by_tiles);
   return {cut.full_items + r - chunk * cut.tiles, chunk, cut.chunks};
@@ -553,7 +565,7 @@ struct HalfK {
   static constexpr int WORDS = BM <= 128 ? 6 : BM + BN <= 320 ? 4 : 2;   // scale words of a row that are held: what the registers allow
 };
 
-template <int BM, int BN, bool QUANT, bool GELU>
+template <int BM, int BN, bool QUARTERS, bool QUANT, bool GELU>
 __global__ __launch_bounds__(512) void gemm_fp8_halfk_kernel(GemmFp8Args g, Grid grid, Cut cut) {
   using C = HalfK<BM, BN>;
   constexpr int MB = BM / 64, NB = BN / 64;            // 32 x 32 blocks of a wave's BM/2 x BN/2 sub-tile
@@ -561,9 +573,17 @@ __global__ __launch_bounds__(512) void gemm_fp8_halfk_kernel(GemmFp8Args g, Grid
   constexpr int RING = C::RING, STAGE = C::STAGE, WORDS = C::WORDS, GROUP = 4 * WORDS;
   constexpr int STEPS = MB * NB, NW = BN == 128 ? 1 : NB;              // scale blocks among a wave's columns
   static_assert(BM % 64 == 0 && BN % 64 == 0 && RING >= 3 && NB >= 2, "tile shape");
-  const CutItem it = cut_item(cut);
+  CutItem it = cut_item<QUARTERS>(cut);
   int m0, n0;
-  if (!origin(grid, it.slot, BM, BN, m0, n0)) return;
+  if (QUARTERS) {
+    if (!origin(grid, it.slot, 256, 256, m0, n0)) return;
+    m0 += (it.chunk & 1) * 128;
+    n0 += (it.chunk >> 1) * 128;
+    if (m0 >= g.m || n0 >= g.n) return;
+    it.n_chunks = 1;
+  } else if (!origin(grid, it.slot, BM, BN, m0, n0)) {
+    return;
+  }
 
   extern __shared__ u32x4_t smem[];
   const uint32_t lds0 = (uint32_t)(size_t)(__attribute__((address_space(3))) void*)smem;
@@ -736,7 +756,7 @@ __global__ __launch_bounds__(512) void gemm_fp8_halfk_kernel(GemmFp8Args g, Grid
   if (it.n_chunks > 1) {
     float* part = cut.parts + ((size_t)(it.slot - cut.full_items) * it.n_chunks + it.chunk) * (BM * BN);
     for (int p = tid; p < BM * BN / 4; p += 512)
-      *reinterpret_cast<floatx4_t*>(part + p * 4) = *reinterpret_cast<const floatx4_t*>(tile + p / (BN / 4) * LDT + p % (BN / 4) * 4);
+      __builtin_nontemporal_store(*reinterpret_cast<const floatx4_t*>(tile + p / (BN / 4) * LDT + p % (BN / 4) * 4), reinterpret_cast<floatx4_t*>(part + p * 4));
     return;
   }
   stream_tile<QUANT, GELU, BM, BN, 512>(g, m0, n0, tid, [&](int ml, int nl, float* v) { ResidIO<float>::load8(tile + ml * LDT + nl, v); });
@@ -902,7 +922,7 @@ hipError_t launch_rows(const GemmFp8Args& g, hipStream_t st) {
 template <int BM, int BN, bool QUANT, bool GELU>
 hipError_t launch_halfk(const GemmFp8Args& g, int chunks, hipStream_t st) {
   static std::atomic<uint64_t> lds_allowed{0};
-  auto kern = gemm_fp8_halfk_kernel<BM, BN, QUANT, GELU>;
+  auto kern = gemm_fp8_halfk_kernel<BM, BN, false, QUANT, GELU>;
   hipError_t e = allow_dynamic_lds(reinterpret_cast<const void*>(kern), HalfK<BM, BN>::LDS, lds_allowed);
   if (e != hipSuccess) return e;
   const Grid grid = make_grid(g, BM, BN);
@@ -912,6 +932,19 @@ hipError_t launch_halfk(const GemmFp8Args& g, int chunks, hipStream_t st) {
   hipLaunchKernelGGL(kern, dim3(full + (slots - full) * chunks), dim3(512), (HalfK<BM, BN>::LDS), st, g, grid, cut);
   if (slots > full)
     hipLaunchKernelGGL((gemm_fp8_fixup_kernel<BM, BN, QUANT, GELU>), dim3((slots - full) * (BM / 16)), dim3(256), 0, st, g, grid, cut);
+  return hipGetLastError();
+}
+
+template <bool QUANT, bool GELU>
+hipError_t launch_quarters(const GemmFp8Args& g, const Grid& grid, hipStream_t st) {
+  static std::atomic<uint64_t> lds_allowed{0};
+  auto kern = gemm_fp8_halfk_kernel<128, 128, true, QUANT, GELU>;
+  constexpr int LDS = HalfK<128, 128>::LDS;
+  hipError_t e = allow_dynamic_lds(reinterpret_cast<const void*>(kern), LDS, lds_allowed);
+  if (e != hipSuccess) return e;
+  const int slots = grid.per_xcd * 8, whole = slots / 256 * 256;
+  const Cut cut = {whole, slots - whole, 4, nullptr, divisor((uint32_t)(slots - whole), 4096), Divisor()};
+  hipLaunchKernelGGL(kern, dim3((slots - whole) * 4), dim3(512), LDS, st, g, grid, cut);
   return hipGetLastError();
 }
 
@@ -927,11 +960,12 @@ hipError_t launch_kind(const GemmFp8Args& g, TileKind kind, int chunks, hipStrea
     case TILE_192:
       if constexpr (QUANT) return hipErrorInvalidValue;                  // a block of 128 columns would lie in two tiles
       else return launch_halfk<192, 192, QUANT, GELU>(g, chunks, st);
-    case TILE_256: return launch_gemm256_fp8<QUANT, GELU>(g, chunks, st);
+    case TILE_256: return launch_gemm256_fp8<QUANT, GELU>(g, chunks, chunks < 0, st);
   }
   return hipErrorInvalidValue;
 }
 
+// chunks: along k, of the tiles of the last round (1: not cut); -1 (256 x 256): they are computed in quarters
 struct TileChoice { TileKind kind; int chunks; };
 
 // The chip runs 256 workgroups at a time: the tiles of a last, partly filled round are cut along k where that pays (the round
