@@ -47,6 +47,7 @@ EXPORTS = (
     "hero_axpy_features", "hero_second_diff_stats", "hero_stability_scores",
     "hero_linear_route", "hero_layer_route", "hero_attention_route",
     "hero_quantize_fp8", "hero_gather_rms_fp8", "hero_linear_fp8", "hero_linear_fp8_quantized",
+    "hero_linear_fp8_route",
 )
 
 
@@ -118,6 +119,7 @@ def load_library(path: Optional[str] = None) -> ctypes.CDLL:
         "hero_attention_route": [I, I, I, I, ctypes.c_size_t, POINTER(I), POINTER(I)],
         "hero_quantize_fp8": [P, I, I, I, I, P, P, P],
         "hero_gather_rms_fp8": [P, I, P, P, I, I, P, c_float, P, P, P, P],
+        "hero_linear_fp8_route": [I, I, I, I, ctypes.c_size_t, POINTER(I), POINTER(I), POINTER(I)],
         "hero_linear_fp8": [P, P, P, P, P, P, I, I, I, I, P, ctypes.c_size_t, P],
         "hero_linear_fp8_quantized": [P, P, P, P, P, P, P, I, I, I, I, P, ctypes.c_size_t, P],
     }
@@ -590,3 +592,10 @@ def hero_linear_fp8_quantized(a, a_scales, w, w_scales, bias, q, scales, act: in
                                 *_scratch_at(scratch, device), calls.stream(device))
     if rc:
         _check(rc)
+
+
+def hero_linear_fp8_route(m: int, n: int, k: int, quantized: bool = False, scratch_bytes: int = 0):
+    """(tile rows, tile columns, what becomes of the last round's tiles) of a product in 8 bits; host only."""
+    out = [c_int32() for _ in range(3)]
+    _check(load_library().hero_linear_fp8_route(m, n, k, int(quantized), scratch_bytes, *(byref(v) for v in out)))
+    return tuple(v.value for v in out)

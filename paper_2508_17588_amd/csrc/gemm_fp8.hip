@@ -968,27 +968,65 @@ hipError_t launch_kind(const GemmFp8Args& g, TileKind kind, int chunks, hipStrea
 // chunks: along k, of the tiles of the last round (1: not cut); -1 (256 x 256): they are computed in quarters
 struct TileChoice { TileKind kind; int chunks; };
 
-// The chip runs 256 workgroups at a time: the tiles of a last, partly filled round are cut along k where that pays (the round
-// then takes ceil(n * s / 256) / s of a tile's time) and the sums fit the scratch.
-int choose_split(const GemmFp8Args& g) {
-  const int slots = ((g.m + 255) / 256 * ((g.n + 255) / 256) + 7) / 8 * 8, n_rem = slots % 256;
-  if (n_rem == 0 || g.scratch == nullptr) return 1;
-  const int stages = (g.k + BK - 1) / BK;
-  const int s_max = (int)std::min<size_t>((size_t)std::min(stages / 16, 8), g.scratch_bytes / ((size_t)n_rem * 262144));
-  double best = 1.0;
-  int split = 1;
-  for (int s = 2; s <= s_max; ++s) {
-    const double t = (double)((n_rem * s + 255) / 256) / s + 0.1 * n_rem / stages * s;
-    if (t < best - 0.02) { best = t; split = s; }
-  }
-  return split;
+// Expected times (us), fitted to 1900 timings of every kind, cut and not, at 48 sizes (1 .. 17776 rows, n 96 .. 7680, k 64 .. 8192)
+// in both result types, those near the fastest weighing most; over these sizes the kind chosen takes 1.4 % longer than the
+// best on average, 20 % at most (4679 x 272 x 4688: uncut where two chunks are better).
+//
+// Tiles: a round of at most 256 of them, one a CU, takes fixed + stages * rate; the rate rises from `low` to `high` as the last
+// CUs come to work and the chip lowers its clock.  Per round at k = 1920: 128 x 128 14.5, 192 x 128 17.4, 192 x 192 22.4,
+// 256 x 256 29.4 us.  [1]: results in 8 bits.
+struct TileCost { int bm, bn; float fixed, low, high; };
+constexpr TileCost TILE_COST[][2] = {{{128, 128, 4.0f, 0.48f, 0.70f}, {128, 128, 5.0f, 0.42f, 0.63f}},
+                                     {{192, 128, 5.3f, 0.70f, 0.81f}, {192, 128, 6.7f, 0.51f, 0.76f}},
+                                     {{192, 192, 7.0f, 0.78f, 1.03f}, {0, 0, 0.f, 0.f, 0.f}},
+                                     {{256, 256, 5.7f, 1.11f, 1.58f}, {256, 256, 5.0f, 1.12f, 1.55f}}};
+// Kernels for few rows: a share for each workgroup of a CU, and the bytes a CU takes in, some 75 a ns.
+struct RowsCost { int rows; float fixed, group, per_mb; };
+constexpr RowsCost ROWS_COST[][2] = {{{16, 0.9f, 0.56f, 13.5f}, {16, 0.f, 1.9f, 13.5f}}, {{32, 0.f, 1.6f, 12.3f}, {32, 0.f, 2.2f, 12.3f}}};
+constexpr float ROWS_STAGE[][2] = {{0.f, 0.06f}, {0.f, 0.10f}};       // of the wave with most stages
+constexpr double FIXUP = 3.7, FIXUP_PER_MB = 0.26, SECOND_LAUNCH = 2.8;
+
+double rounds_cost(const TileCost& c, int64_t items, double stages) {
+  const double rem = (double)(items % 256) / 256.0;
+  return (double)(items / 256) * (c.fixed + stages * c.high) +
+         (rem > 0 ? c.fixed + stages * (c.low + rem * rem * rem * (c.high - c.low)) : 0.0);
 }
 
+// stages a chunk of a cut tile has at least: fewer do not cover the start of its pipeline
+constexpr int LEAST_STAGES = 8, MOST_CHUNKS = 8;
+
 TileChoice choose_tile(const GemmFp8Args& g) {
-  if (g.m <= 16 && rows_stages(g) <= ROWS_STAGES) return {TILE_16, 1};
-  if (g.m <= 32 && rows_stages(g) <= ROWS_STAGES) return {TILE_32, 1};
-  if (g.m <= 512) return {TILE_128, 1};
-  return {TILE_256, choose_split(g)};
+  const int quant = g.out.q != nullptr ? 1 : 0, stages = (g.k + BK - 1) / BK;
+  TileChoice choice = {TILE_256, 1};
+  double best = 1e30;
+  auto consider = [&](TileKind kind, int chunks, double t) {
+    if (t < best) { best = t; choice = {kind, chunks}; }
+  };
+  const int columns = quant ? 128 : 16;
+  for (int r = 0; r < 2 && rows_stages(g) <= ROWS_STAGES; ++r) {
+    const RowsCost& c = ROWS_COST[r][quant];
+    const int64_t groups = (int64_t)((g.n + columns - 1) / columns) * ((g.m + c.rows - 1) / c.rows), a_cu = (groups + 255) / 256;
+    if (groups > (1 << 20)) continue;
+    consider(r == 0 ? TILE_16 : TILE_32, 1, c.fixed + ROWS_STAGE[r][quant] * rows_stages(g) + c.group * a_cu +
+             c.per_mb * 1e-6 * (double)a_cu * stages * (c.rows + columns) * BK);
+  }
+  for (int kind = TILE_128; kind <= TILE_256; ++kind) {
+    const TileCost& c = TILE_COST[kind - TILE_128][quant];
+    if (c.bm == 0) continue;
+    const int64_t tiles = (int64_t)((g.m + c.bm - 1) / c.bm) * ((g.n + c.bn - 1) / c.bn);
+    const int64_t slots = (tiles + 7) / 8 * 8, whole = slots / 256 * 256, rem = slots - whole;
+    consider((TileKind)kind, 1, rounds_cost(c, tiles, stages));
+    if (rem == 0) continue;
+    const double before = rounds_cost(c, whole, stages);
+    if (kind == TILE_256)
+      consider(TILE_256, -1, before + (whole > 0 ? SECOND_LAUNCH : 0.0) + rounds_cost(TILE_COST[0][quant], 4 * (tiles - whole), stages));
+    for (int s = 2; s <= MOST_CHUNKS && stages / s >= LEAST_STAGES && g.scratch != nullptr; ++s) {
+      const size_t bytes = (size_t)rem * s * c.bm * c.bn * 4;
+      if (bytes > g.scratch_bytes) break;
+      consider((TileKind)kind, s, before + rounds_cost(c, rem * s, (double)stages / s) + FIXUP + FIXUP_PER_MB * 1e-6 * (double)bytes);
+    }
+  }
+  return choice;
 }
 
 }  // namespace
@@ -1001,4 +1039,12 @@ hipError_t launch_gemm_fp8(const GemmFp8Args& g, hipStream_t st) {
   const TileChoice t = choose_tile(g);
   if (g.out.q) return g.gelu ? launch_kind<true, true>(g, t.kind, t.chunks, st) : launch_kind<true, false>(g, t.kind, t.chunks, st);
   return g.gelu ? launch_kind<false, true>(g, t.kind, t.chunks, st) : launch_kind<false, false>(g, t.kind, t.chunks, st);
+}
+
+void gemm_fp8_route(const GemmFp8Args& g, int* tile_m, int* tile_n, int* last) {
+  const TileChoice t = choose_tile(g);
+  static const int bm[] = {16, 32, 128, 192, 192, 256}, bn[] = {16, 16, 128, 128, 192, 256};
+  *tile_m = bm[t.kind];
+  *tile_n = t.kind <= TILE_32 && g.out.q ? 128 : bn[t.kind];
+  *last = t.chunks;
 }

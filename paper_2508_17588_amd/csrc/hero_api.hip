@@ -43,6 +43,8 @@ bool aligned16(std::initializer_list<const void*> ptrs) {
   return true;
 }
 
+// 8-bit operands are addressed with 32-bit byte offsets
+bool fp8_offsets_fit(int64_t m, int64_t n, int64_t k) { return (m + 512) * k < (int64_t)1 << 32 && (n + 512) * k < (int64_t)1 << 32; }
 // 512-element pieces of rows are counted in 31 bits
 bool fp8_rows_fit(int64_t n_rows, int64_t columns) { return n_rows * ((columns + 511) / 512) < (int64_t)1 << 31; }
 
@@ -1128,13 +1130,30 @@ static int linear_fp8(GemmFp8Args& g, int32_t act, size_t scratch_bytes, hipStre
     return fail(HERO_ERR_INVALID_ARG, "null pointer");
   if (g.k % 16 != 0 || g.n % 16 != 0) return fail(HERO_ERR_SHAPE, "k and n must be multiples of 16");
   if (act != 0 && act != 1) return fail(HERO_ERR_INVALID_ARG, "act must be 0 or 1");
-  if (((int64_t)g.m + 512) * g.k >= (int64_t)1 << 32 || ((int64_t)g.n + 512) * g.k >= (int64_t)1 << 32)
+  if (!fp8_offsets_fit(g.m, g.n, g.k))
     return fail(HERO_ERR_SHAPE, "(m + 512) * k and (n + 512) * k must stay below 2^32 (32-bit operand offsets)");
   if (!aligned16({g.a, g.w, g.bias, g.c, g.out.q, g.scratch}) || (((uintptr_t)g.a_scales | (uintptr_t)g.w_scales | (uintptr_t)g.out.scales) & 3))
     return fail(HERO_ERR_INVALID_ARG, "a, w, bias, the result and scratch must be 16-byte aligned, scales 4-byte aligned");
   g.gelu = act != 0;
   g.scratch_bytes = g.scratch ? scratch_bytes : 0;
   HIP_TRY(launch_gemm_fp8(g, st));
+  return HERO_OK;
+}
+
+// (the route only asks whether there is scratch and how much, and whether the result is in 8 bits: any address stands for it)
+int hero_linear_fp8_route(int32_t m, int32_t n, int32_t k, int32_t quantized, size_t scratch_bytes, int32_t* tile_m,
+                          int32_t* tile_n, int32_t* last) {
+  if (!tile_m || !tile_n || !last) return fail(HERO_ERR_INVALID_ARG, "output pointer is null");
+  if (m <= 0 || n <= 0 || k <= 0) return fail(HERO_ERR_INVALID_ARG, "bad sizes");
+  if (k % 16 != 0 || n % 16 != 0) return fail(HERO_ERR_SHAPE, "k and n must be multiples of 16");
+  if (!fp8_offsets_fit(m, n, k)) return fail(HERO_ERR_SHAPE, "beyond the 32-bit operand offsets");
+  GemmFp8Args g;
+  uint8_t any = 0;
+  float any_scratch = 0.f;
+  g.m = m; g.n = n; g.k = k;
+  g.out.q = quantized ? &any : nullptr;
+  if (scratch_bytes > 0) { g.scratch = &any_scratch; g.scratch_bytes = scratch_bytes; }
+  gemm_fp8_route(g, tile_m, tile_n, last);
   return HERO_OK;
 }
 

@@ -230,3 +230,6 @@ struct GemmFp8Args {
   size_t scratch_bytes = 0;
 };
 hipError_t launch_gemm_fp8(const GemmFp8Args& g, hipStream_t st);
+// the tile launch_gemm_fp8 takes, and what becomes of those of the last round (1: computed like the others; s > 1: cut in s along k;
+// -1: computed in quarters)
+void gemm_fp8_route(const GemmFp8Args& g, int* tile_m, int* tile_n, int* last);

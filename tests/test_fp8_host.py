@@ -83,6 +83,21 @@ def test_linear_refusals(lib, quantized):
     assert rc(m=0, a=None, sa=None, c=None, s=None) == B.HERO_OK
 
 
+def test_route(lib):
+    t = [ctypes.c_int32() for _ in range(3)]
+    p = [ctypes.byref(v) for v in t]
+    assert lib.hero_linear_fp8_route(0, 64, 64, 0, 0, *p) == lib.hero_linear_fp8_route(1, 64, 64, 0, 0, None, *p[1:]) == B.HERO_ERR_INVALID_ARG
+    assert lib.hero_linear_fp8_route(1, 24, 64, 0, 0, *p) == lib.hero_linear_fp8_route(1 << 20, 64, 4096, 0, 0, *p) == B.HERO_ERR_SHAPE
+    for m, n, k, q in ((1, 1920, 7680, False), (17776, 7680, 1920, True), (550, 720, 3008, False), (4, 16, 1 << 20, True)):
+        # without scratch nothing is cut, and a little more of it never makes a tile that does not fit
+        assert B.hero_linear_fp8_route(m, n, k, q, 0)[2] in (1, -1)
+        for scratch in (1 << 10, 1 << 22, 1 << 26):
+            bm, bn, last = B.hero_linear_fp8_route(m, n, k, q, scratch)
+            if last > 1:
+                tiles = -(-m // bm) * -(-n // bn)
+                assert -(-tiles // 8) * 8 % 256 * last * bm * bn * 4 <= scratch
+
+
 def test_binding_refuses_what_does_not_fit():
     q, s = B.empty_fp8(4, 64, device="cpu")
     x = torch.zeros(4, 64)

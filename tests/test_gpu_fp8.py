@@ -239,6 +239,32 @@ def test_linear_many_tiles(m, n, k, quantized):
     run_linear(a, w, bias, 0, quantized, scratch=torch.empty(64 << 20, dtype=torch.uint8, device="cuda"), rows=rows)
 
 
+# Every kernel that a product can go to: the tile and what becomes of the last round's tiles, with 64 MiB of scratch
+SCRATCH = 64 << 20
+ROUTES = [
+    (1, 16, 16, False, (16, 16, 1)), (9, 7520, 1936, False, (16, 16, 1)), (65, 832, 16, False, (32, 16, 1)), (61, 1920, 7696, False, (32, 16, 1)),
+    (161, 1888, 16, False, (128, 128, 1)), (2047, 2048, 2032, False, (128, 128, 1)), (550, 720, 3008, False, (128, 128, 3)),
+    (137, 2608, 8160, False, (192, 128, 8)), (16590, 160, 16, False, (192, 128, 1)), (1217, 4688, 528, False, (192, 192, 1)),
+    (7262, 160, 6688, False, (192, 192, 5)), (626, 8864, 16, False, (256, 256, 1)), (17311, 784, 144, False, (256, 256, -1)),
+    (2958, 7024, 3776, False, (256, 256, 2)),
+    (1, 16, 16, True, (16, 128, 1)), (13, 1936, 1936, True, (16, 128, 1)), (4135, 16, 16, True, (32, 128, 1)), (1, 16, 7792, True, (128, 128, 7)),
+    (137, 2608, 8160, True, (192, 128, 6)), (16505, 176, 400, True, (192, 128, 1)), (16706, 272, 5792, True, (192, 128, 5)),
+    (16590, 160, 16, True, (256, 256, 1)), (14604, 1056, 544, True, (256, 256, -1)), (1406, 4144, 5088, True, (256, 256, 2)),
+    (10879, 1296, 4848, True, (256, 256, 4)),
+]
+
+
+@pytest.mark.parametrize("m,n,k,quantized,route", ROUTES)
+def test_linear_every_kernel(m, n, k, quantized, route):
+    say(f"linear {m} x {n} x {k} quantized {quantized}: {route}")
+    assert B.hero_linear_fp8_route(m, n, k, quantized, SCRATCH) == route
+    a, w, bias = operands(m, n, k)
+    rows = torch.unique(torch.cat([torch.randint(0, m, (120,), generator=torch.Generator().manual_seed(m)), torch.tensor([0, m - 1])]))
+    scratch = torch.full((SCRATCH // 4,), float("nan"), device="cuda")
+    for act in (0, 1):
+        run_linear(a, w, bias, act, quantized, scratch=scratch, rows=rows)
+
+
 @pytest.mark.parametrize("quantized", [False, True])
 def test_linear_without_bias(quantized):
     say(f"linear without bias, quantized {quantized}")
