@@ -368,7 +368,7 @@ int hero_stability_scores(const double* variances, int32_t n_layers, double* sco
  * 0; never below byte 0), every element rounded to nearest, ties to even; NaN and infinities become NaN elements and do not
  * count for the scale. */
 #define HERO_FP8_BLOCK 128
-#define HERO_FP8_SCALE_PITCH(columns) (((columns) + 511) / 512 * 4)
+#define HERO_FP8_SCALE_PITCH(columns) (((columns) / 512 + ((columns) % 512 != 0)) * 4)
 
 /* x [n_rows, columns] (fp32 or bf16) in 8 bits: out_q [n_rows, columns], out_scales [ceil(n_rows / block_rows), pitch].
  * block_rows: 1 (activations) or 128 (weights).  The buffers of an empty problem may be NULL. */
@@ -389,7 +389,8 @@ int hero_gather_rms_fp8(const void* dev_x, int32_t x_dtype, const void* dev_add_
  * hero_linear_fp8_quantized in 8 bits (out_q [M,N], out_scales [M, pitch(N)]), ready to be the next product's A.
  * Products are added up in fp32; the matrix instructions align the products of eight neighbouring k to the largest of them,
  * which keeps 13 bits below its leading one.
- * Pointers 16-byte aligned (scales 4-byte).  (M + 512) * K and (N + 512) * K must stay below 2^32, else HERO_ERR_SHAPE.
+ * Pointers 16-byte aligned (scales 4-byte).  (M + 512) * K and (N + 512) * K must stay below 2^32, N below
+ * 2^23 and the result within 2^23 - 16 tiles of 128 x 128, else HERO_ERR_SHAPE.
  * dev_scratch: optional (NULL and 0: none) device memory of the caller, 16-byte aligned, any contents, any size, as for
  * hero_linear_scratch: some problems are faster with it.  Calls that share it must not overlap. */
 int hero_linear_fp8(const void* dev_a, const void* dev_a_scales, const void* dev_w, const void* dev_w_scales,

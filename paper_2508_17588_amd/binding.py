@@ -510,6 +510,11 @@ def _at(t, dtype, device, least: int, name: str) -> int:
     return t.data_ptr()
 
 
+def _fits_int32(rows: int, columns: int) -> None:
+    if rows >= 1 << 31 or columns >= 1 << 31:
+        raise ValueError("sizes must stay below 2^31")
+
+
 def _scratch_at(scratch, device):
     if scratch is None:
         return 0, 0
@@ -532,6 +537,7 @@ def hero_quantize_fp8(x, q, scales, block_rows: int = 1):
     if block_rows != 1 and block_rows != FP8_BLOCK:
         raise ValueError("block_rows must be 1 or 128")
     rows, columns = x.shape
+    _fits_int32(rows, columns)
     code = _x_code(calls, x)
     rc = calls.quantize(_at(x, x.dtype, device, 0, "x"), code, rows, columns, block_rows,
                         _at(q, calls.e4m3, device, rows * columns, "q"),
@@ -545,6 +551,7 @@ def hero_gather_rms_fp8(x, add, rows, n_rows: int, gain, eps: float, q, scales, 
     """q, scales: (x + add)[rows] * gain / rms in 8 bits; sum (optional, x's type) takes (x + add)[rows] itself."""
     calls, device = _fp8(x)
     hidden, size = x.shape[-1], x.numel()
+    _fits_int32(n_rows, hidden)
     if gain.numel() != hidden or (add is not None and add.numel() != size) or (rows is None and size < n_rows * hidden):
         raise ValueError("shape mismatch")
     if sum is not None and rows is not None and sum.untyped_storage().data_ptr() == x.untyped_storage().data_ptr():
@@ -567,6 +574,8 @@ def _linear_fp8_operands(calls, device, a, a_scales, w, w_scales, bias):
     (m, k), (n, k_w) = a.shape, w.shape
     if k_w != k or (bias is not None and bias.numel() != n):
         raise ValueError("shape mismatch")
+    _fits_int32(m, k)
+    _fits_int32(n, k)
     pitch = fp8_scale_pitch(k)
     return m, n, k, (_at(a, calls.e4m3, device, 0, "a"), _at(a_scales, calls.e8m0, device, m * pitch, "a_scales"),
                      _at(w, calls.e4m3, device, 0, "w"), _at(w_scales, calls.e8m0, device, -(-n // FP8_BLOCK) * pitch, "w_scales"),

@@ -6,7 +6,7 @@
 // bound by HBM: one pass, every byte read and written once.  Elements and sums are stored past the caches (nontemporal):
 // 17776 x 1920 of bf16 with add and sum 50.5 -> 45.2 us, weight blocks 7680 x 1920 10.5 -> 9.1; nontemporal loads are
 // slower (the same rms over 4485 listed rows 12.4 -> 14.1 us).  A float32 copy of 137 MB runs at 5.9 to 6.3 TB/s here.
-#include <type_traits>
+#include <algorithm>
 
 #include "fp8_device.h"
 #include "hero_kernels.h"
@@ -164,7 +164,7 @@ __global__ __launch_bounds__(256) void quantize_blocks_kernel(const XT* __restri
 
 template <typename XT>
 hipError_t rms_dispatch(const RmsFp8Args& a, hipStream_t st) {
-  const int pieces = (a.hidden + PIECE - 1) / PIECE, pitch = fp8_scale_pitch(a.hidden);
+  const int pitch = fp8_scale_pitch(a.hidden), pieces = pitch / 4;
 #define LAUNCH(I, W)                                                                                               \
   hipLaunchKernelGGL((rms_fp8_kernel<XT, I, W>), dim3(W == 1 ? (a.n_rows + 3) / 4 : a.n_rows), dim3(W == 1 ? 256 : 64 * W), 0, \
                      st, a, pitch)
@@ -181,30 +181,58 @@ hipError_t rms_dispatch(const RmsFp8Args& a, hipStream_t st) {
   return hipGetLastError();
 }
 
+template <typename XT>
+hipError_t quantize_dispatch(const XT* x, int n_rows, int columns, int block_rows, const Fp8Out& out, hipStream_t st) {
+  const int pitch = fp8_scale_pitch(columns);
+  if (block_rows == 1) {
+    const int64_t pieces = (int64_t)n_rows * (pitch / 4);
+    hipLaunchKernelGGL(quantize_rows_kernel<XT>, dim3((unsigned)((pieces + 3) / 4)), dim3(256), 0, st, x, pieces, columns,
+                       pitch / 4, out);
+  } else {
+    hipLaunchKernelGGL(quantize_blocks_kernel<XT>, dim3(columns / 128 + (columns % 128 != 0), (n_rows + 127) / 128), dim3(256), 0, st, x,
+                       n_rows, columns, pitch, out);
+  }
+  return hipGetLastError();
+}
+
+// A launch has fewer than 2^32 threads in x and 2^16 workgroups in y: more rows than these go to several launches.
+constexpr int LAUNCH_ROWS = 1 << 21;       // (of 1024 threads at most, or 2^14 rows of blocks)
+
 }  // namespace
 
-hipError_t launch_gather_rms_fp8(const RmsFp8Args& a, hipStream_t st) {
-  if (a.n_rows <= 0) return hipSuccess;
-  if (a.hidden <= 0 || a.hidden % 16 != 0) return hipErrorInvalidValue;
-  return a.x_fp32 ? rms_dispatch<float>(a, st) : rms_dispatch<bf16_t>(a, st);
+hipError_t launch_gather_rms_fp8(const RmsFp8Args& all, hipStream_t st) {
+  if (all.hidden <= 0 || all.hidden % 16 != 0) return hipErrorInvalidValue;
+  hipError_t e = hipSuccess;
+  for (int r = 0; r < all.n_rows && e == hipSuccess; r += std::min(LAUNCH_ROWS, all.n_rows - r)) {
+    RmsFp8Args a = all;
+    const int64_t done = (int64_t)r * a.hidden, x_bytes = done * (a.x_fp32 ? 4 : 2);
+    a.n_rows = std::min(LAUNCH_ROWS, all.n_rows - r);
+    if (a.rows) a.rows += r;
+    else {
+      a.x = static_cast<const char*>(a.x) + x_bytes;
+      if (a.add) a.add += done;
+    }
+    if (a.sum) a.sum = static_cast<char*>(a.sum) + x_bytes;
+    a.out.q += done;
+    a.out.scales += (int64_t)r * fp8_scale_pitch(a.hidden);
+    e = a.x_fp32 ? rms_dispatch<float>(a, st) : rms_dispatch<bf16_t>(a, st);
+  }
+  return e;
 }
 
 hipError_t launch_quantize_fp8(const void* x, bool x_fp32, int n_rows, int columns, int block_rows, const Fp8Out& out,
                                hipStream_t st) {
-  if (n_rows <= 0 || columns <= 0) return hipSuccess;
-  if (columns % 16 != 0) return hipErrorInvalidValue;
-  if (block_rows == 1) {
-    const int row_pieces = (columns + PIECE - 1) / PIECE;
-    const int64_t pieces = (int64_t)n_rows * row_pieces, groups = (pieces + 3) / 4;
-    if (groups > 0x7fffffff) return hipErrorInvalidValue;
-    const dim3 grid((unsigned)groups);
-    if (x_fp32) hipLaunchKernelGGL(quantize_rows_kernel<float>, grid, dim3(256), 0, st, static_cast<const float*>(x), pieces, columns, row_pieces, out);
-    else hipLaunchKernelGGL(quantize_rows_kernel<bf16_t>, grid, dim3(256), 0, st, static_cast<const bf16_t*>(x), pieces, columns, row_pieces, out);
-    return hipGetLastError();
-  }
-  const dim3 grid((columns + 127) / 128, (n_rows + 127) / 128);
+  if (columns <= 0 || columns % 16 != 0) return hipErrorInvalidValue;
   const int pitch = fp8_scale_pitch(columns);
-  if (x_fp32) hipLaunchKernelGGL(quantize_blocks_kernel<float>, grid, dim3(256), 0, st, static_cast<const float*>(x), n_rows, columns, pitch, out);
-  else hipLaunchKernelGGL(quantize_blocks_kernel<bf16_t>, grid, dim3(256), 0, st, static_cast<const bf16_t*>(x), n_rows, columns, pitch, out);
-  return hipGetLastError();
+  // (64 threads a piece: 2^31 a launch)
+  const int most = block_rows == 1 ? std::max(1, std::min(LAUNCH_ROWS, (1 << 25) / (pitch / 4))) : LAUNCH_ROWS;
+  hipError_t e = hipSuccess;
+  for (int r = 0; r < n_rows && e == hipSuccess; r += std::min(most, n_rows - r)) {
+    const int64_t done = (int64_t)r * columns;
+    const int rows = std::min(most, n_rows - r);
+    const Fp8Out o = {out.q + done, out.scales + (int64_t)(r / block_rows) * pitch};
+    e = x_fp32 ? quantize_dispatch(static_cast<const float*>(x) + done, rows, columns, block_rows, o, st)
+               : quantize_dispatch(static_cast<const bf16_t*>(x) + done, rows, columns, block_rows, o, st);
+  }
+  return e;
 }

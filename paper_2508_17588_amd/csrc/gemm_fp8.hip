@@ -1034,8 +1034,8 @@ TileChoice choose_tile(const GemmFp8Args& g) {
 hipError_t launch_gemm_fp8(const GemmFp8Args& g, hipStream_t st) {
   if (g.m <= 0 || g.n <= 0) return hipSuccess;
   if (g.k <= 0 || g.k % 16 != 0 || g.n % 16 != 0) return hipErrorInvalidValue;
-  // operands are addressed with 32-bit byte offsets
-  if (((int64_t)g.m + 512) * g.k >= (int64_t)1 << 32 || ((int64_t)g.n + 512) * g.k >= (int64_t)1 << 32) return hipErrorInvalidValue;
+  // operands, and 256 rows of a result, are addressed with 32-bit byte offsets
+  if (((int64_t)g.m + 512) * g.k >= (int64_t)1 << 32 || ((int64_t)g.n + 512) * g.k >= (int64_t)1 << 32 || g.n >= 1 << 23) return hipErrorInvalidValue;
   const TileChoice t = choose_tile(g);
   if (g.out.q) return g.gelu ? launch_kind<true, true>(g, t.kind, t.chunks, st) : launch_kind<true, false>(g, t.kind, t.chunks, st);
   return g.gelu ? launch_kind<false, true>(g, t.kind, t.chunks, st) : launch_kind<false, false>(g, t.kind, t.chunks, st);

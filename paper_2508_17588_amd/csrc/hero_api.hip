@@ -43,8 +43,14 @@ bool aligned16(std::initializer_list<const void*> ptrs) {
   return true;
 }
 
-// 8-bit operands are addressed with 32-bit byte offsets
-bool fp8_offsets_fit(int64_t m, int64_t n, int64_t k) { return (m + 512) * k < (int64_t)1 << 32 && (n + 512) * k < (int64_t)1 << 32; }
+// 8-bit operands are addressed with 32-bit byte offsets, and so are 256 rows of a result; a launch has less than 2^32 threads
+const char* fp8_misfit(int64_t m, int64_t n, int64_t k) {
+  if ((m + 512) * k >= (int64_t)1 << 32 || (n + 512) * k >= (int64_t)1 << 32)
+    return "(m + 512) * k and (n + 512) * k must stay below 2^32 (32-bit operand offsets)";
+  if (n >= 1 << 23) return "n must stay below 2^23 (32-bit offsets in 256 rows of the result)";
+  if ((m + 127) / 128 * ((n + 127) / 128) > (1 << 23) - 16) return "the result has more than 2^23 - 16 tiles of 128 x 128";
+  return nullptr;
+}
 // 512-element pieces of rows are counted in 31 bits
 bool fp8_rows_fit(int64_t n_rows, int64_t columns) { return n_rows * ((columns + 511) / 512) < (int64_t)1 << 31; }
 
@@ -1130,8 +1136,7 @@ static int linear_fp8(GemmFp8Args& g, int32_t act, size_t scratch_bytes, hipStre
     return fail(HERO_ERR_INVALID_ARG, "null pointer");
   if (g.k % 16 != 0 || g.n % 16 != 0) return fail(HERO_ERR_SHAPE, "k and n must be multiples of 16");
   if (act != 0 && act != 1) return fail(HERO_ERR_INVALID_ARG, "act must be 0 or 1");
-  if (!fp8_offsets_fit(g.m, g.n, g.k))
-    return fail(HERO_ERR_SHAPE, "(m + 512) * k and (n + 512) * k must stay below 2^32 (32-bit operand offsets)");
+  if (const char* why = fp8_misfit(g.m, g.n, g.k)) return fail(HERO_ERR_SHAPE, "%s", why);
   if (!aligned16({g.a, g.w, g.bias, g.c, g.out.q, g.scratch}) || (((uintptr_t)g.a_scales | (uintptr_t)g.w_scales | (uintptr_t)g.out.scales) & 3))
     return fail(HERO_ERR_INVALID_ARG, "a, w, bias, the result and scratch must be 16-byte aligned, scales 4-byte aligned");
   g.gelu = act != 0;
@@ -1146,7 +1151,7 @@ int hero_linear_fp8_route(int32_t m, int32_t n, int32_t k, int32_t quantized, si
   if (!tile_m || !tile_n || !last) return fail(HERO_ERR_INVALID_ARG, "output pointer is null");
   if (m <= 0 || n <= 0 || k <= 0) return fail(HERO_ERR_INVALID_ARG, "bad sizes");
   if (k % 16 != 0 || n % 16 != 0) return fail(HERO_ERR_SHAPE, "k and n must be multiples of 16");
-  if (!fp8_offsets_fit(m, n, k)) return fail(HERO_ERR_SHAPE, "beyond the 32-bit operand offsets");
+  if (const char* why = fp8_misfit(m, n, k)) return fail(HERO_ERR_SHAPE, "%s", why);
   GemmFp8Args g;
   uint8_t any = 0;
   float any_scratch = 0.f;

@@ -194,7 +194,7 @@ hipError_t launch_attention(const AttnArgs& a, hipStream_t st);
 void attention_route(const AttnArgs& a, int* queries, int* key_ranges);
 
 // 8-bit rows and weights: e4m3 elements, one E8M0 scale a block of 128 (include/hero.h)
-constexpr int fp8_scale_pitch(int columns) { return (columns + 511) / 512 * 4; }
+constexpr int fp8_scale_pitch(int columns) { return (columns / 512 + (columns % 512 != 0)) * 4; }
 
 struct Fp8Out {
   uint8_t* q = nullptr;            // [rows, columns]

@@ -105,8 +105,8 @@ def rms(x, add, rows, gain, eps):
     return h / torch.sqrt((h * h).mean(dim=1, keepdim=True) + eps) * gain.double().cpu(), h
 
 
-# The norm in fp32, relative to y: h 1, its square 3, at most 46 additions of positive numbers (32 in a lane, 6 over the
-# lanes, 8 waves), the division 1 and eps 1: 52 units of 2^-24 on the mean square, 26 on its root; the reciprocal root 4;
+# The norm in fp32, relative to y: h 1, its square 3, at most 46 additions of positive numbers (16 in a lane, 6 over the
+# lanes, 16 waves: 38), the division 1 and eps 1: 52 units of 2^-24 on the mean square, 26 on its root; the reciprocal root 4;
 # two products 2.  33 in all.
 RMS_ERROR = 33 * U32
 

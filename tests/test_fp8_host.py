@@ -83,6 +83,25 @@ def test_linear_refusals(lib, quantized):
     assert rc(m=0, a=None, sa=None, c=None, s=None) == B.HERO_OK
 
 
+@pytest.mark.parametrize("m,n,k,what", [(300, 1 << 23, 16, b"2^23"), (1, (1 << 23) - 16, 16, None), (1 << 27, 1 << 20, 16, b"tiles"),
+                                        (1 << 28, 16, 16, b"2^32"), ((1 << 28) - 528, 16, 16, None)])
+def test_largest_products(lib, m, n, k, what):
+    if what is None:
+        assert B.hero_linear_fp8_route(m, n, k)
+        return
+    out = [ctypes.byref(ctypes.c_int32()) for _ in range(3)]
+    assert lib.hero_linear_fp8_route(m, n, k, 0, 0, *out) == B.HERO_ERR_SHAPE and what in lib.hero_last_error()
+    assert lib.hero_linear_fp8(P, P, P, P, P, P, m, n, k, 0, None, 0, None) == B.HERO_ERR_SHAPE and what in lib.hero_last_error()
+
+
+def test_binding_refuses_sizes_past_31_bits():
+    """(A size that the C call's argument cannot hold would otherwise arrive as its low 32 bits.)"""
+    for sizes in ((1 << 31, 16), (1 << 32, 16), (16, 1 << 31)):
+        with pytest.raises(ValueError, match="2\\^31"):
+            B._fits_int32(*sizes)
+    B._fits_int32((1 << 31) - 1, 16)
+
+
 def test_route(lib):
     t = [ctypes.c_int32() for _ in range(3)]
     p = [ctypes.byref(v) for v in t]

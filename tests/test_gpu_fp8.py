@@ -330,6 +330,93 @@ def test_padding_bytes_of_scales_are_not_used():
     assert torch.equal(got, want)
 
 
+# ---- beyond one launch, beyond 32 bits -------------------------------------------------------------
+
+MANY = (1 << 21) + 133
+
+
+def some_rows(rows, *borders):
+    """The first rows, the last and those on both sides of the borders."""
+    near = [torch.arange(max(0, b - 3), min(rows, b + 4)) for b in (0, rows, *borders)]
+    return torch.cat(near).unique()
+
+
+@pytest.mark.parametrize("rows,columns,borders", [(MANY, 16, (1 << 21,)), (9, 1 << 22, ()), (70000, 1040, (1 << 16,)), (300, 16 << 20, (256,))])
+def test_quantize_of_many_rows(rows, columns, borders):
+    say(f"quantize {rows} x {columns}")
+    x = torch.randn(rows, columns, device="cuda", dtype=torch.bfloat16, generator=torch.Generator("cuda").manual_seed(1))
+    q, s = room(rows, columns)
+    B.hero_quantize_fp8(x, q, s)
+    torch.cuda.synchronize()
+    q, s = written(q, s, rows)
+    pick, last = some_rows(rows, *borders), max(0, (columns - 1024) // 512 * 512)
+    code, byte = F.quantized(x[pick.cuda(), last:].cpu().double())
+    assert torch.equal(F.codes(q.view(torch.uint8)[pick.cuda(), last:]), code)
+    assert torch.equal(s.view(torch.uint8)[pick.cuda(), last // 128: F.pitch(columns)].cpu(), byte)
+
+
+@pytest.mark.parametrize("rows", [MANY, (1 << 23) + 1])
+def test_quantize_blocks_of_many_rows(rows):
+    say(f"quantize {rows} x 16 in blocks")
+    x = torch.randn(rows, 16, device="cuda", dtype=torch.bfloat16, generator=torch.Generator("cuda").manual_seed(1))
+    q, s = room(rows, 16, 128)
+    B.hero_quantize_fp8(x, q, s, 128)
+    torch.cuda.synchronize()
+    q, s = written(q, s, rows, 128)
+    for b in (0, (1 << 14) - 1, 1 << 14, s.shape[0] - 2, s.shape[0] - 1):
+        part = slice(128 * b, min(rows, 128 * b + 128))
+        code, byte = F.quantized(x[part].cpu().double(), 128)
+        assert torch.equal(F.codes(q[part]), code) and torch.equal(s[b: b + 1].view(torch.uint8).cpu(), byte)
+
+
+@pytest.mark.parametrize("listed", [False, True])
+def test_rms_of_many_rows(listed):
+    say(f"rms {MANY} x 32 listed {listed}")
+    gen = torch.Generator("cuda").manual_seed(2)
+    x = torch.randn(MANY, 32, device="cuda", generator=gen)
+    add = torch.randn(MANY, 32, device="cuda", generator=gen).bfloat16()
+    rows = torch.arange(MANY - 1, -1, -1, dtype=torch.int32, device="cuda") if listed else None
+    gain = torch.ones(32, dtype=torch.bfloat16)
+    total = torch.full((MANY + 2, 32), 7.0, device="cuda")
+    q, s = room(MANY, 32)
+    B.hero_gather_rms_fp8(x, add, rows, MANY, gain.cuda(), 1e-6, q, s, total)
+    torch.cuda.synchronize()
+    q, s = written(q, s, MANY)
+    pick = some_rows(MANY, 1 << 21).cuda()
+    src = rows[pick].long() if listed else pick
+    y, h = F.rms(x[src].cpu(), add[src].cpu(), None, gain, 1e-6)
+    F.check_fp8(q.view(torch.uint8)[pick].view(q.dtype), s.view(torch.uint8)[pick].view(s.dtype), y, F.RMS_ERROR * y.abs(), "rms")
+    assert bool((total[MANY:] == 7.0).all())
+    assert torch.equal(total[pick], x[src] + add[src].float())
+
+
+@pytest.mark.parametrize("m,n,quantized", [(270000, 8192, False), (530000, 8192, True), (300, (8 << 20) - 16, False), (560, (8 << 20) - 16, True)])
+def test_results_past_4_gib(m, n, quantized):
+    say(f"linear {m} x {n} x 16 quantized {quantized}")
+    a, w, bias = operands(m, n, 16)
+    (aq, as_), (wq, ws) = a, w
+    border = (1 << 32) // (n * (1 if quantized else 2))
+    rows, cols = some_rows(m, border), slice(max(0, (n - 1600) // 512 * 512), n)
+    if quantized:
+        out = room(m, n)
+        B.hero_linear_fp8_quantized(aq, as_, wq, ws, bias, *out)
+        torch.cuda.synchronize()
+        out = written(*out, m)
+    else:
+        c = torch.full((m + 2, n), 7.0, dtype=torch.bfloat16, device="cuda")
+        B.hero_linear_fp8(aq, as_, wq, ws, bias, c)
+        torch.cuda.synchronize()
+        assert bool((c[m:] == 7.0).all()), "rows behind the last"
+    at = rows.cuda()
+    some_a = F.values(aq.view(torch.uint8)[at].view(aq.dtype), as_.view(torch.uint8)[at].view(as_.dtype))
+    v, off = F.linear(some_a, F.values(wq[cols], ws[cols.start // 128:], 128), bias[cols], 0)
+    if quantized:
+        scales = out[1].view(torch.uint8)[at][:, cols.start // 128: F.pitch(n)].view(torch.float8_e8m0fnu)
+        F.check_fp8(out[0].view(torch.uint8)[at][:, cols].view(torch.float8_e4m3fn), scales, v, off, "past 4 GiB")
+    else:
+        F.check_bf16(c[at][:, cols], v, off, "past 4 GiB")
+
+
 # ---- together --------------------------------------------------------------------------------------
 
 def branch(x, add, rows, n, gain, w1, b1, w2, b2, room_, scratch=None):
