@@ -109,6 +109,7 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES) void rms_fp8_kernel(
   }
 }
 
+// A piece to a wave (17776 x 1920 of bf16: 19.2 us, 5.3 TB/s; four pieces a wave 25 us)
 template <typename XT>
 __global__ __launch_bounds__(256) void quantize_rows_kernel(const XT* __restrict__ x, int64_t pieces, int columns,
                                                             int row_pieces, Fp8Out out) {
@@ -125,6 +126,7 @@ __global__ __launch_bounds__(256) void quantize_rows_kernel(const XT* __restrict
 }
 
 // 128 x 128 blocks: a workgroup a block, 16 rows of it at a time, all of it in registers until its largest magnitude is known
+// (7680 x 1920 of bf16: 9.1 us, 4.8 TB/s; 5760 x 1920 of fp32 10.4 us, 5.3 TB/s)
 template <typename XT>
 __global__ __launch_bounds__(256) void quantize_blocks_kernel(const XT* __restrict__ x, int n_rows, int columns,
                                                               int pitch, Fp8Out out) {

@@ -18,14 +18,20 @@ namespace {
 // ------------------------------------------------------------------------------------------
 // Large problems: 256 x 256 tile, eight waves (two per SIMD) of 64 x 128, K walked in stages of 128 (one scale block, one
 // 128-byte line per row) through LDS rings of three A slots and two W slots (all 160 KB of a CU) that are filled by direct
-// global -> LDS loads, W one stage and A two stages ahead; LDS rows of 128 B whose eight 16-byte chunks are
-// XOR-swizzled with (row/2)%8.  One barrier a stage.  In bytes a stage is that of a bf16 kernel with k steps of 64, and takes
-// the matrix pipe as long (16 MFMAs of 64 cycles a wave), at twice the flops.
+// global -> LDS loads, A two stages ahead, W in halves of a stage of which three are on their way; LDS rows of 128 B whose eight
+// 16-byte chunks are XOR-swizzled with (row/2)%8.  A barrier each half stage.  In bytes a stage is that of a bf16 kernel with
+// k steps of 64, and takes the matrix pipe as long (16 MFMAs of 64 cycles a wave), at twice the flops.
+// Bound by the matrix pipes at the clock that the chip's power allows: 8192^3 runs at 2.73 PFLOP/s on random data and at 3.9
+// on zeros (a loop of these MFMAs on registers: 3.2 to 3.8 and 4.6).  17776 x 7680 x 1920 takes 225 to 235 us (2.2 to 2.3
+// PFLOP/s; with GELU into 8 bits 251 to 265, whose epilogues the pipes wait for), 17776 x 1920 x 7680 230.
 //  * A wave's 128 columns are one scale block of the weight and, in 8-bit results, one block of the output row: its scale is
 //    found without leaving the wave.
-//  * The four MFMAs of a stage's last two W fragments run after the next barrier, while the first fragments of the new stage
-//    arrive; within a stage a fragment is read four MFMAs ahead of its use, so four W fragments and two pairs of A
-//    fragments are all that is held (64 registers beside 128 accumulators).
+//  * The last four MFMAs of a half stage run after the next barrier, while the first fragments behind it arrive; a fragment is
+//    read four MFMAs ahead of its use, so four W fragments and two pairs of A fragments are all that is held (64 registers
+//    beside 128 accumulators).
+//  * Workgroups walk over the tiles: the next tile's first fills go out before a result is stored.  (17776 x 7680 x 1920: 264 us
+//    with W filled a whole stage ahead, 249 in halves, 241 with sums that begin with the bias and tile places found without
+//    divisions, the rest from the last round's quarters.)
 //  * Scale bytes of GROUP stages lie in registers, shifted down a byte a stage; those of the next group are asked for at the
 //    start of a group, since the wait for them is a wait for every fill in flight.
 // ------------------------------------------------------------------------------------------
@@ -434,7 +440,8 @@ __global__ __launch_bounds__(512) void gemm256_fp8_kernel(Args256 args) {
   }
 }
 
-// Adds up the chunks of the cut tiles and stores the result: a one-wave workgroup to each 64 x 128 part of a tile.
+// Adds up the chunks of the cut tiles and stores the result: a one-wave workgroup to each 64 x 128 part of a tile.  Bound by the
+// partial sums, read once and past the caches, 0.26 us a MB.
 template <bool QUANT, bool GELU>
 __global__ __launch_bounds__(64) void gemm256_fp8_fixup_kernel(GemmFp8Args g, Grid grid, Split sk) {
   const int tile = blockIdx.x >> 3, wave = blockIdx.x & 7, lane = threadIdx.x;
@@ -556,6 +563,8 @@ __device__ __forceinline__ CutItem cut_item(const Cut& cut) {
 // sub-tile is then large (few LDS reads a flop) with two waves on every SIMD.  Stages go global -> LDS into a ring of RING
 // slots, filled RING - 1 stages ahead, one barrier a stage; a slot holds the BM rows of A, then the BN rows of W.  As in the
 // 256 x 256 kernel the MFMAs of a stage's last W fragment run after the next barrier, while the first fragments arrive.
+// Bound by what a CU takes in, 65 to 75 KB/us by such fills: 128 x 128 takes 4 us and 0.48 us a stage of 32 KB (with all 256 CUs
+// at work 0.7), 192 x 192 7 and 0.78 to 1.03 of 48 KB.  4485 x 1920 x 7680, 240 tiles of 192 x 192: 66 us, 2.0 PFLOP/s.
 template <int BM, int BN>
 struct HalfK {
   static constexpr int STAGE = (BM + BN) * 128;                          // bytes
@@ -762,7 +771,8 @@ __global__ __launch_bounds__(512) void gemm_fp8_halfk_kernel(GemmFp8Args g, Grid
   stream_tile<QUANT, GELU, BM, BN, 512>(g, m0, n0, tid, [&](int ml, int nl, float* v) { ResidIO<float>::load8(tile + ml * LDT + nl, v); });
 }
 
-// Adds up the chunks of cut tiles and stores the result; 16 rows of a tile to a workgroup.
+// Adds up the chunks of cut tiles and stores the result; 16 rows of a tile to a workgroup, so that small problems have some
+// 256 of them (226 x 1920 x 7680 in six chunks, 12 MB: 4.2 us).
 template <int BM, int BN, bool QUANT, bool GELU>
 __global__ __launch_bounds__(256) void gemm_fp8_fixup_kernel(GemmFp8Args g, Grid grid, Cut cut) {
   constexpr int ROWS = 16;
@@ -788,6 +798,7 @@ __global__ __launch_bounds__(256) void gemm_fp8_fixup_kernel(GemmFp8Args g, Grid
 // 16 columns (8-bit results: 128, a block), v_mfma_scale_f32_16x16x128_f8f6f4 (A fragment: lane holds row lane%16 and a
 // quarter of 128 k; accumulator register i of a lane is row 4*(lane/16) + i, column lane%16).  Each wave has its own share
 // of k (8-bit results: its own 16 columns) and a ring of its own, so there is no barrier until the sums meet in LDS.
+// Bound by latency and by the weight's bytes: 1 x 7680 x 1920 takes 3.7 us back to back, 4 TB/s.
 template <int R, int RING>
 struct FewRows {
   static constexpr int STAGE = (16 * R + 16) * 128;                       // bytes: the rows of A, then 16 of W
