@@ -401,8 +401,7 @@ int hero_linear_fp8_quantized(const void* dev_a, const void* dev_a_scales, const
                               int32_t k, int32_t act, void* dev_scratch, size_t scratch_bytes, void* stream);
 
 /* Which kernel a product in 8 bits goes to, with scratch_bytes of scratch (host only; see hero_linear_route).  A tile of 16
- * or 32 rows: the kernel for few rows, whose waves share k.  *last: what becomes of the tiles of the last, partly filled
- * round: 1 computed like the others, s > 1 cut in s chunks along k, -1 computed in quarters. */
+ * to 64 rows: the kernel whose waves share k.  *last: what becomes of the tiles of the last, partly filled round: 1 computed like the others, s > 1 cut in s chunks along k, -1 computed in quarters. */
 int hero_linear_fp8_route(int32_t m, int32_t n, int32_t k, int32_t quantized, size_t scratch_bytes, int32_t* tile_m,
                           int32_t* tile_n, int32_t* last);
 

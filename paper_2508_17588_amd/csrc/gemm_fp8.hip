@@ -794,35 +794,41 @@ __global__ __launch_bounds__(256) void gemm_fp8_fixup_kernel(GemmFp8Args g, Grid
   });
 }
 
-// Few rows: what counts is that the weight's bytes are all asked for at once.  A workgroup of eight waves has 16 * R rows and
-// 16 columns (8-bit results: 128, a block), v_mfma_scale_f32_16x16x128_f8f6f4 (A fragment: lane holds row lane%16 and a
-// quarter of 128 k; accumulator register i of a lane is row 4*(lane/16) + i, column lane%16).  Each wave has its own share
-// of k (8-bit results: its own 16 columns) and a ring of its own, so there is no barrier until the sums meet in LDS.
-// Bound by latency and by the weight's bytes: 1 x 7680 x 1920 takes 3.7 us back to back, 4 TB/s.
-template <int R, int RING>
-struct FewRows {
-  static constexpr int STAGE = (16 * R + 16) * 128;                       // bytes: the rows of A, then 16 of W
+// Few tiles: what counts is that operands are asked for early, many at once, and taken in by every CU.  A workgroup has 16 * R rows and
+// 16 * C columns (8-bit results: 128, a block) and its waves share k, each with a ring of RING slots of its own, so there is no
+// barrier until the sums meet in LDS.  v_mfma_scale_f32_16x16x128_f8f6f4 (A fragment: lane holds row lane%16 and a quarter of
+// 128 k; accumulator register i of a lane is row 4*(lane/16) + i, column lane%16): a stage of 128 k is one step.
+// Bound by what a CU takes in, 80 to 90 KB/us, after a start of 2 to 3 us: 226 x 1920 x 1920 in tiles of 32 x 64 takes 5.4 us (tiles
+// of 128 x 128 11.8, of 32 x 16 10.2), 128 x 4096 x 4096 8.2 (17.3 cut along k, 16.7), 226 x 1920 x 7680 12.2 (17.2, 22.2);
+// 1 x 7680 x 1920 in tiles of 16 x 16 3.7 us back to back, 4 TB/s of weights.  A slot each for eight waves is as good as three
+// each for four.  Operands loaded straight into registers took twice as long: such a load touches 16 lines where one into LDS
+// touches eight.
+template <int R, int C, int WAVES, int RING>
+struct SharedK {
+  static constexpr int STAGE = 16 * (R + C) * 128;                        // bytes: the rows of A, then those of W
   static constexpr int WAVE = RING * STAGE + (R + 1) * 1024;               // and scale bytes of 64 stages: of the rows of A, of W
-  static constexpr int LDS = 8 * WAVE;
+  static constexpr int LDT = 16 * C + 4, SUMS = WAVES * 16 * R * LDT * 4;
+  static constexpr int LDS = WAVES * WAVE > SUMS ? WAVES * WAVE : SUMS;
 };
-constexpr int ROWS_STAGES = 60;      // most stages of a wave: 64, as its scale bytes begin on a whole word
 
-template <int R, int RING, bool QUANT, bool GELU>
-__global__ __launch_bounds__(512) void gemm_fp8_rows_kernel(GemmFp8Args g, int tiles_n) {
-  using C = FewRows<R, RING>;
-  constexpr int STAGE = C::STAGE, NF = 2 * R + 2, COLS = QUANT ? 128 : 16;
+constexpr int SHARED_STAGES = 60;    // most stages of a wave: 64, as its scale bytes begin on a whole word
+
+template <int R, int C, int WAVES, int RING, bool QUANT, bool GELU>
+__global__ __launch_bounds__(64 * WAVES) void gemm_fp8_shared_kernel(GemmFp8Args g, Grid grid) {
+  using S = SharedK<R, C, WAVES, RING>;
+  constexpr int STAGE = S::STAGE, NF = 2 * (R + C), LDT = S::LDT;
+  int m0, n0;
+  if (!origin(grid, blockIdx.x, 16 * R, 16 * C, m0, n0)) return;
   extern __shared__ u32x4_t smem[];
   const int tid = threadIdx.x, lane = tid & 63, lr = lane & 15, lq = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int tile_n = blockIdx.x % tiles_n, m0 = blockIdx.x / tiles_n * (16 * R), n0 = tile_n * COLS;
-  const int wn0 = n0 + (QUANT ? wave * 16 : 0);
-  const uint32_t ring = __builtin_amdgcn_readfirstlane((uint32_t)(size_t)(__attribute__((address_space(3))) void*)smem) + wave * C::WAVE;
+  const uint32_t ring = __builtin_amdgcn_readfirstlane((uint32_t)(size_t)(__attribute__((address_space(3))) void*)smem) + wave * S::WAVE;
   const uint32_t scales = ring + RING * STAGE;
   const uint32_t row_bytes = (uint32_t)g.k;
   const u32x4_t rsA = rsrc_words(g.a, (uint32_t)g.m * row_bytes);
   const u32x4_t rsB = rsrc_words(g.w, (uint32_t)g.n * row_bytes);
   const int n_stages = (g.k + BK - 1) / BK;
-  const int begin = QUANT ? 0 : wave * n_stages / 8, end = QUANT ? n_stages : (wave + 1) * n_stages / 8;
+  const int begin = wave * n_stages / WAVES, end = (wave + 1) * n_stages / WAVES;
   // scale bytes: lane l brings those of row l/4, stages 16 * (l%4) .. +15 from the word of `begin` on; W's one row in lanes 0-3
   const int pitch = fp8_scale_pitch(g.k), scale_begin = begin & ~3;
   {
@@ -831,20 +837,22 @@ __global__ __launch_bounds__(512) void gemm_fp8_rows_kernel(GemmFp8Args g, int t
     const uint32_t at = (uint32_t)(scale_begin + (lane & 3) * 16);
 #pragma unroll
     for (int i = 0; i < R; ++i) lds_fill(rsSA, scales + i * 1024, (uint32_t)(m0 + 16 * i + (lane >> 2)) * (uint32_t)pitch + at);
-    lds_fill(rsSW, scales + R * 1024, lane < 4 ? (uint32_t)(wn0 / 128) * (uint32_t)pitch + at : 0xFFFFFFF0u);
+    lds_fill(rsSW, scales + R * 1024, lane < 4 ? (uint32_t)(n0 / 128) * (uint32_t)pitch + at : 0xFFFFFFF0u);
   }
   auto fill = [&](int slot, int stage) {
 #pragma unroll
     for (int i = 0; i < NF; ++i) {
       const int row = i * 8 + (lane >> 3), chunk = (lane & 7) ^ ((row >> 1) & 7);
       const uint32_t past = stage * BK + chunk * 16 >= g.k ? 0xFFFFFFF0u : 0u;
-      const uint32_t v = (uint32_t)(i < 2 * R ? m0 + row : wn0 + row - 16 * R) * row_bytes + chunk * 16;
+      const uint32_t v = (uint32_t)(i < 2 * R ? m0 + row : n0 + row - 16 * R) * row_bytes + chunk * 16;
       lds_fill(i < 2 * R ? rsA : rsB, ring + (uint32_t)slot * STAGE + i * 1024, v | past, (uint32_t)stage * BK);
     }
   };
-  floatx4_t acc[R];
+  floatx4_t acc[R][C];
 #pragma unroll
-  for (int i = 0; i < R; ++i) acc[i] = floatx4_t{0.f, 0.f, 0.f, 0.f};
+  for (int i = 0; i < R; ++i)
+#pragma unroll
+    for (int j = 0; j < C; ++j) acc[i][j] = floatx4_t{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
   for (int s = 0; s < RING; ++s)
     if (begin + s < end) fill(s, begin + s);
@@ -860,21 +868,22 @@ __global__ __launch_bounds__(512) void gemm_fp8_rows_kernel(GemmFp8Args g, int t
   for (int t = begin; t < end; ++t) {
     // the fills of the stages after this one may still be in flight
     const int newer = min(RING - 1, end - 1 - t);
-    if (newer == 3) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(3 * NF) : "memory");
-    else if (newer == 2) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(2 * NF) : "memory");
-    else if (newer == 1) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(NF) : "memory");
+    if (RING > 3 && newer == 3) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(RING > 3 ? 3 * NF : 0) : "memory");
+    else if (RING > 2 && newer == 2) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(RING > 2 ? 2 * NF : 0) : "memory");
+    else if (RING > 1 && newer == 1) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(RING > 1 ? NF : 0) : "memory");
     else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-    static_assert(RING <= 4, "counts above");
+    static_assert(RING <= 4 && (RING - 1) * NF < 64, "counts above");
     const uint32_t base = ring + (uint32_t)slot * STAGE, s = scales + (uint32_t)(t - scale_begin);
-    const i32x8_t w = frag(base + 2048 * R);
     const int scale_w = *(lds_byte_t)(size_t)(s + R * 1024);
-    i32x8_t a[R];
+    i32x8_t a[R], w[C];
     int scale_a[R];
 #pragma unroll
     for (int i = 0; i < R; ++i) {
       a[i] = frag(base + 2048 * i);
       scale_a[i] = *(lds_byte_t)(size_t)(s + i * 1024 + lr * 64);
     }
+#pragma unroll
+    for (int j = 0; j < C; ++j) w[j] = frag(base + 2048 * (R + j));
     if (t + RING < end) {
       asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");                  // the slot has been read
       __builtin_amdgcn_sched_barrier(0);
@@ -882,23 +891,25 @@ __global__ __launch_bounds__(512) void gemm_fp8_rows_kernel(GemmFp8Args g, int t
     }
 #pragma unroll
     for (int i = 0; i < R; ++i)
-      acc[i] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(w, a[i], acc[i], 0, 0, 0, scale_w, 0, scale_a[i]);
+#pragma unroll
+      for (int j = 0; j < C; ++j)
+        acc[i][j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(w[j], a[i], acc[i][j], 0, 0, 0, scale_w, 0, scale_a[i]);
     slot = slot == RING - 1 ? 0 : slot + 1;
   }
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");                        // (a wave without stages has scale bytes on their way)
   __syncthreads();                       // every wave has read its last stage: no fill is in flight
-  // acc[i][e] = C[m0 + 16i + lr][wn0 + 4lq + e]
+  // acc[i][j][e] = C[m0 + 16i + lr][n0 + 16j + 4lq + e]
   float* tile = reinterpret_cast<float*>(smem);
-  constexpr int LDT = COLS + 4, COPIES = QUANT ? 1 : 8;
-  static_assert(COPIES * 16 * R * LDT * 4 <= C::LDS, "sums");
 #pragma unroll
   for (int i = 0; i < R; ++i)
-    *reinterpret_cast<floatx4_t*>(tile + ((QUANT ? 0 : wave * 16 * R) + 16 * i + lr) * LDT + (QUANT ? wave * 16 : 0) + 4 * lq) = acc[i];
+#pragma unroll
+    for (int j = 0; j < C; ++j)
+      *reinterpret_cast<floatx4_t*>(tile + (wave * 16 * R + 16 * i + lr) * LDT + 16 * j + 4 * lq) = acc[i][j];
   __syncthreads();
-  stream_tile<QUANT, GELU, 16 * R, COLS, 512>(g, m0, n0, tid, [&](int ml, int nl, float* v) {
+  stream_tile<QUANT, GELU, 16 * R, 16 * C, 64 * WAVES>(g, m0, n0, tid, [&](int ml, int nl, float* v) {
     ResidIO<float>::load8(tile + ml * LDT + nl, v);
 #pragma unroll
-    for (int c = 1; c < COPIES; ++c) {
+    for (int c = 1; c < WAVES; ++c) {
       float w[8];
       ResidIO<float>::load8(tile + (c * 16 * R + ml) * LDT + nl, w);
 #pragma unroll
@@ -907,27 +918,18 @@ __global__ __launch_bounds__(512) void gemm_fp8_rows_kernel(GemmFp8Args g, int t
   });
 }
 
-template <int R, int RING, bool QUANT, bool GELU>
-hipError_t launch_rows_ring(const GemmFp8Args& g, hipStream_t st) {
+template <int R, int C, int WAVES, int RING, bool QUANT, bool GELU>
+hipError_t launch_shared(const GemmFp8Args& g, hipStream_t st) {
   static std::atomic<uint64_t> lds_allowed{0};
-  constexpr int LDS = FewRows<R, RING>::LDS;
-  auto kern = gemm_fp8_rows_kernel<R, RING, QUANT, GELU>;
+  constexpr int LDS = SharedK<R, C, WAVES, RING>::LDS;
+  static_assert(LDS <= 163840, "LDS of a CU");
+  if (((g.k + BK - 1) / BK + WAVES - 1) / WAVES > SHARED_STAGES) return hipErrorInvalidValue;
+  auto kern = gemm_fp8_shared_kernel<R, C, WAVES, RING, QUANT, GELU>;
   hipError_t e = allow_dynamic_lds(reinterpret_cast<const void*>(kern), LDS, lds_allowed);
   if (e != hipSuccess) return e;
-  const int tiles_n = QUANT ? (g.n + 127) / 128 : g.n / 16, tiles_m = (g.m + 16 * R - 1) / (16 * R);
-  hipLaunchKernelGGL(kern, dim3(tiles_n * tiles_m), dim3(512), LDS, st, g, tiles_n);
+  const Grid grid = make_grid(g, 16 * R, 16 * C);
+  hipLaunchKernelGGL(kern, dim3(grid.per_xcd * 8), dim3(64 * WAVES), LDS, st, g, grid);
   return hipGetLastError();
-}
-// stages of the wave that has most
-int rows_stages(const GemmFp8Args& g) {
-  const int stages = (g.k + BK - 1) / BK;
-  return g.out.q ? stages : (stages + 7) / 8;
-}
-// Two slots a wave where they hold all its stages (two workgroups to a CU), else as many as the LDS takes
-template <int R, bool QUANT, bool GELU>
-hipError_t launch_rows(const GemmFp8Args& g, hipStream_t st) {
-  if (rows_stages(g) > ROWS_STAGES) return hipErrorInvalidValue;
-  return rows_stages(g) <= 2 ? launch_rows_ring<R, 2, QUANT, GELU>(g, st) : launch_rows_ring<R, R == 1 ? 4 : 2, QUANT, GELU>(g, st);
 }
 
 template <int BM, int BN, bool QUANT, bool GELU>
@@ -959,13 +961,29 @@ hipError_t launch_quarters(const GemmFp8Args& g, const Grid& grid, hipStream_t s
   return hipGetLastError();
 }
 
-enum TileKind { TILE_16, TILE_32, TILE_128, TILE_192x128, TILE_192, TILE_256 };
+// TILE_16 to TILE_64x128: whose waves share k; 8-bit results: 16 x 128, 32 x 128 and 64 x 128
+enum TileKind { TILE_16, TILE_32, TILE_32x64, TILE_64, TILE_64x128, TILE_128, TILE_192x128, TILE_192, TILE_256 };
 
 template <bool QUANT, bool GELU>
 hipError_t launch_kind(const GemmFp8Args& g, TileKind kind, int chunks, hipStream_t st) {
+  const int stages = (g.k + BK - 1) / BK;
   switch (kind) {
-    case TILE_16: return launch_rows<1, QUANT, GELU>(g, st);
-    case TILE_32: return launch_rows<2, QUANT, GELU>(g, st);
+    case TILE_16:
+      // one tile's weights: two slots a wave, and two workgroups to a CU, where they hold all its stages (1 x 7680 x 1920: 5.1 us with three
+      // inputs in turns, 6.6 with four slots), else four (149 x 816 x 3008 8.2 -> 6.8).  A block of 128 columns: four waves with two
+      // slots for the fewest stages (8160 columns, two stages: 3.9 us, eight waves with a slot 4.2), else eight (5 x 304 x 7344: 11.1, 12.8)
+      if constexpr (QUANT) return stages <= 4 ? launch_shared<1, 8, 4, 2, QUANT, GELU>(g, st) : launch_shared<1, 8, 8, 1, QUANT, GELU>(g, st);
+      else return stages <= 16 ? launch_shared<1, 1, 8, 2, QUANT, GELU>(g, st) : launch_shared<1, 1, 8, 4, QUANT, GELU>(g, st);
+    case TILE_32:
+      if constexpr (QUANT) return launch_shared<2, 8, 6, 1, QUANT, GELU>(g, st);
+      else return launch_shared<2, 2, 8, 2, QUANT, GELU>(g, st);
+    case TILE_32x64:
+      if constexpr (QUANT) return hipErrorInvalidValue;
+      else return launch_shared<2, 4, 8, 1, QUANT, GELU>(g, st);
+    case TILE_64:
+      if constexpr (QUANT) return hipErrorInvalidValue;
+      else return launch_shared<4, 4, 4, 2, QUANT, GELU>(g, st);
+    case TILE_64x128: return launch_shared<4, 8, 4, 1, QUANT, GELU>(g, st);
     case TILE_128: return launch_halfk<128, 128, QUANT, GELU>(g, chunks, st);
     case TILE_192x128: return launch_halfk<192, 128, QUANT, GELU>(g, chunks, st);
     case TILE_192:
@@ -979,9 +997,10 @@ hipError_t launch_kind(const GemmFp8Args& g, TileKind kind, int chunks, hipStrea
 // chunks: along k, of the tiles of the last round (1: not cut); -1 (256 x 256): they are computed in quarters
 struct TileChoice { TileKind kind; int chunks; };
 
-// Expected times (us), fitted to 1900 timings of every kind, cut and not, at 48 sizes (1 .. 17776 rows, n 96 .. 7680, k 64 .. 8192)
-// in both result types, those near the fastest weighing most; over these sizes the kind chosen takes 1.4 % longer than the
-// best on average, 20 % at most (4679 x 272 x 4688: uncut where two chunks are better).
+// Expected times (us), fitted to timings of every kind, cut and not, in both result types, those near the fastest weighing
+// most: the tiles from 128 x 128 on to 1900 at 48 sizes (1 .. 17776 rows, n 96 .. 7680, k 64 .. 8192), those whose waves share k to
+// 1000 at 72 (1 .. 2553 rows, n 16 .. 8160, k 192 .. 7872).  At the latter the kind chosen takes 2.4 % longer than the best of all
+// kinds on average, 26 % at most (2 x 416 x 7168 in 8 bits: seven chunks where 16 x 128 tiles are better).
 //
 // Tiles: a round of at most 256 of them, one a CU, takes fixed + stages * rate; the rate rises from `low` to `high` as the last
 // CUs come to work and the chip lowers its clock.  Per round at k = 1920: 128 x 128 14.5, 192 x 128 17.4, 192 x 192 22.4,
@@ -991,10 +1010,13 @@ constexpr TileCost TILE_COST[][2] = {{{128, 128, 4.0f, 0.48f, 0.70f}, {128, 128,
                                      {{192, 128, 5.3f, 0.70f, 0.81f}, {192, 128, 6.7f, 0.51f, 0.76f}},
                                      {{192, 192, 7.0f, 0.78f, 1.03f}, {0, 0, 0.f, 0.f, 0.f}},
                                      {{256, 256, 5.7f, 1.11f, 1.58f}, {256, 256, 5.0f, 1.12f, 1.55f}}};
-// Kernels for few rows: a share for each workgroup of a CU, and the bytes a CU takes in, some 75 a ns.
-struct RowsCost { int rows; float fixed, group, per_mb; };
-constexpr RowsCost ROWS_COST[][2] = {{{16, 0.9f, 0.56f, 13.5f}, {16, 0.f, 1.9f, 13.5f}}, {{32, 0.f, 1.6f, 12.3f}, {32, 0.f, 2.2f, 12.3f}}};
-constexpr float ROWS_STAGE[][2] = {{0.f, 0.06f}, {0.f, 0.10f}};       // of the wave with most stages
+// Tiles whose waves share k: the stages of a wave, a share for each workgroup of a CU, and the bytes that a CU takes in, some 85 a ns.
+struct SharedCost { int bm, bn, waves; float fixed, stage, group, per_mb; };
+constexpr SharedCost SHARED_COST[][2] = {{{16, 16, 8, 2.4f, 0.f, 0.42f, 13.1f}, {16, 128, 8, 1.1f, 0.f, 2.2f, 11.1f}},
+                                         {{32, 32, 8, 1.3f, 0.12f, 1.7f, 10.5f}, {32, 128, 6, 0.8f, 0.f, 3.3f, 11.6f}},
+                                         {{32, 64, 8, 1.1f, 0.f, 2.2f, 11.6f}, {0, 0, 0, 0.f, 0.f, 0.f, 0.f}},
+                                         {{64, 64, 4, 0.4f, 0.24f, 3.0f, 12.3f}, {0, 0, 0, 0.f, 0.f, 0.f, 0.f}},
+                                         {{64, 128, 4, 0.f, 0.53f, 4.2f, 10.9f}, {64, 128, 4, 0.f, 0.44f, 5.3f, 9.6f}}};
 constexpr double FIXUP = 3.7, FIXUP_PER_MB = 0.26, SECOND_LAUNCH = 2.8;
 
 double rounds_cost(const TileCost& c, int64_t items, double stages) {
@@ -1013,13 +1035,13 @@ TileChoice choose_tile(const GemmFp8Args& g) {
   auto consider = [&](TileKind kind, int chunks, double t) {
     if (t < best) { best = t; choice = {kind, chunks}; }
   };
-  const int columns = quant ? 128 : 16;
-  for (int r = 0; r < 2 && rows_stages(g) <= ROWS_STAGES; ++r) {
-    const RowsCost& c = ROWS_COST[r][quant];
-    const int64_t groups = (int64_t)((g.n + columns - 1) / columns) * ((g.m + c.rows - 1) / c.rows), a_cu = (groups + 255) / 256;
-    if (groups > (1 << 20)) continue;
-    consider(r == 0 ? TILE_16 : TILE_32, 1, c.fixed + ROWS_STAGE[r][quant] * rows_stages(g) + c.group * a_cu +
-             c.per_mb * 1e-6 * (double)a_cu * stages * (c.rows + columns) * BK);
+  for (int kind = TILE_16; kind <= TILE_64x128; ++kind) {
+    const SharedCost& c = SHARED_COST[kind][quant];
+    if (c.bm == 0 || (stages + c.waves - 1) / c.waves > SHARED_STAGES) continue;
+    const int64_t tiles = (int64_t)((g.m + c.bm - 1) / c.bm) * ((g.n + c.bn - 1) / c.bn), a_cu = (tiles + 255) / 256;
+    if (tiles > (1 << 20)) continue;
+    consider((TileKind)kind, 1, c.fixed + c.stage * ((stages + c.waves - 1) / c.waves) + c.group * a_cu +
+             c.per_mb * 1e-6 * (double)a_cu * stages * (c.bm + c.bn) * BK);
   }
   for (int kind = TILE_128; kind <= TILE_256; ++kind) {
     const TileCost& c = TILE_COST[kind - TILE_128][quant];
@@ -1054,8 +1076,8 @@ hipError_t launch_gemm_fp8(const GemmFp8Args& g, hipStream_t st) {
 
 void gemm_fp8_route(const GemmFp8Args& g, int* tile_m, int* tile_n, int* last) {
   const TileChoice t = choose_tile(g);
-  static const int bm[] = {16, 32, 128, 192, 192, 256}, bn[] = {16, 16, 128, 128, 192, 256};
-  *tile_m = bm[t.kind];
-  *tile_n = t.kind <= TILE_32 && g.out.q ? 128 : bn[t.kind];
+  const int quant = g.out.q != nullptr ? 1 : 0;
+  *tile_m = t.kind < TILE_128 ? SHARED_COST[t.kind][quant].bm : TILE_COST[t.kind - TILE_128][quant].bm;
+  *tile_n = t.kind < TILE_128 ? SHARED_COST[t.kind][quant].bn : TILE_COST[t.kind - TILE_128][quant].bn;
   *last = t.chunks;
 }
