@@ -479,7 +479,8 @@ class _Fp8Calls:
         self.linear, self.linear_quantized = lib.hero_linear_fp8, lib.hero_linear_fp8_quantized
         self.e4m3, self.e8m0, self.bf16, self.fp32, self.int32 = (torch.float8_e4m3fn, torch.float8_e8m0fnu, torch.bfloat16,
                                                                   torch.float32, torch.int32)
-        self.device = torch.cuda.current_device
+        # (asked for only once a tensor lies on a device: the runtime is up)
+        self.device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
         try:
             self.stream = torch._C._cuda_getCurrentRawStream
         except AttributeError:      # a torch without it
