@@ -451,7 +451,8 @@ def hero_stability_scores(variances):
 
 # ---- 8-bit linear layers ------------------------------------------------------------------
 # Elements are torch.float8_e4m3fn tensors [rows, columns], scales torch.float8_e8m0fnu tensors
-# [rows, fp8_scale_pitch(columns)] (a weight's: [ceil(rows / 128), ...]).
+# [rows, fp8_scale_pitch(columns)] (a weight's: [ceil(rows / 128), ...]).  On a few rows a call is over as soon as its launch,
+# some 3 us, and checking its tensors here took as long again: csrc/fp8_binding.cpp does it.
 
 FP8_BLOCK = 128
 
@@ -468,138 +469,55 @@ def empty_fp8(rows: int, columns: int, block_rows: int = 1, device="cuda"):
             torch.empty(-(-rows // block_rows), fp8_scale_pitch(columns), dtype=torch.float8_e8m0fnu, device=device))
 
 
-class _Fp8Calls:
-    """What the calls below look up on every call, looked up once: a call on a few rows is over sooner than its checks
-    were (one row of 1920 channels, hero_gather_rms_fp8: 8.5 -> 6.7 us)."""
-
-    def __init__(self):
-        import torch
-        lib = load_library()
-        self.quantize, self.rms = lib.hero_quantize_fp8, lib.hero_gather_rms_fp8
-        self.linear, self.linear_quantized = lib.hero_linear_fp8, lib.hero_linear_fp8_quantized
-        self.e4m3, self.e8m0, self.bf16, self.fp32, self.int32 = (torch.float8_e4m3fn, torch.float8_e8m0fnu, torch.bfloat16,
-                                                                  torch.float32, torch.int32)
-        # (asked for only once a tensor lies on a device: the runtime is up)
-        self.device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
-        try:
-            self.stream = torch._C._cuda_getCurrentRawStream
-        except AttributeError:      # a torch without it
-            self.stream = lambda device: torch.cuda.current_stream(device).cuda_stream
-
-
 _fp8_calls = None
 
 
-def _fp8(first):
-    """The calls, and the current device, on which `first` has to lie (all tensors of a call do)."""
+def _fp8():
+    """The module that checks the tensors of these calls and makes them, with the addresses of the library's entry points."""
     global _fp8_calls
     if _fp8_calls is None:
-        _fp8_calls = _Fp8Calls()
-    if not first.is_cuda:
-        raise TypeError("not a device tensor")
-    return _fp8_calls, _fp8_calls.device()
-
-
-def _at(t, dtype, device, least: int, name: str) -> int:
-    """Address of a contiguous tensor of that type on the current device that has room for `least` elements."""
-    if t.dtype is not dtype or not t.is_contiguous():
-        raise TypeError(f"{name} must be a contiguous {dtype} device tensor")
-    if t.get_device() != device:
-        raise ValueError(f"{name} lies on {t.device}, but the current device is cuda:{device}")
-    if t.numel() < least:
-        raise ValueError(f"{name} is too small")
-    return t.data_ptr()
-
-
-def _fits_int32(rows: int, columns: int) -> None:
-    if rows >= 1 << 31 or columns >= 1 << 31:
-        raise ValueError("sizes must stay below 2^31")
-
-
-def _scratch_at(scratch, device):
-    if scratch is None:
-        return 0, 0
-    return _at(scratch, scratch.dtype, device, 0, "scratch"), scratch.numel() * scratch.element_size()
-
-
-def _x_code(calls, x) -> int:
-    if x.dtype is calls.fp32:
-        return DTYPE_FP32
-    if x.dtype is calls.bf16:
-        return DTYPE_BF16
-    raise TypeError(f"unsupported activation dtype {x.dtype}")
+        import torch
+        try:
+            from . import _fp8_binding
+        except ImportError as e:
+            raise ImportError(f"{e}: build it with `python -m paper_2508_17588_amd.build`") from e
+        lib = load_library()
+        # (asked for only once a tensor lies on a device: the runtime is up)
+        device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
+        stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+        if stream is None:          # a torch without it
+            stream = lambda device: torch.cuda.current_stream(device).cuda_stream
+        address = lambda call: ctypes.cast(call, c_void_p).value
+        _fp8_binding.init(address(lib.hero_quantize_fp8), address(lib.hero_gather_rms_fp8), address(lib.hero_linear_fp8),
+                          address(lib.hero_linear_fp8_quantized), device, stream)
+        _fp8_calls = _fp8_binding
+    return _fp8_calls
 
 
 def hero_quantize_fp8(x, q, scales, block_rows: int = 1):
     """x [rows, columns] (float32 or bfloat16) in 8 bits; block_rows 128: as a weight."""
-    calls, device = _fp8(x)
-    if x.dim() != 2:
-        raise ValueError("x must be [rows, columns]")
-    if block_rows != 1 and block_rows != FP8_BLOCK:
-        raise ValueError("block_rows must be 1 or 128")
-    rows, columns = x.shape
-    _fits_int32(rows, columns)
-    code = _x_code(calls, x)
-    rc = calls.quantize(_at(x, x.dtype, device, 0, "x"), code, rows, columns, block_rows,
-                        _at(q, calls.e4m3, device, rows * columns, "q"),
-                        _at(scales, calls.e8m0, device, -(-rows // block_rows) * fp8_scale_pitch(columns), "scales"),
-                        calls.stream(device))
+    rc = (_fp8_calls or _fp8()).quantize(x, q, scales, block_rows)
     if rc:
         _check(rc)
 
 
 def hero_gather_rms_fp8(x, add, rows, n_rows: int, gain, eps: float, q, scales, sum=None):
     """q, scales: (x + add)[rows] * gain / rms in 8 bits; sum (optional, x's type) takes (x + add)[rows] itself."""
-    calls, device = _fp8(x)
-    hidden, size = x.shape[-1], x.numel()
-    _fits_int32(n_rows, hidden)
-    if gain.numel() != hidden or (add is not None and add.numel() != size) or (rows is None and size < n_rows * hidden):
-        raise ValueError("shape mismatch")
-    if sum is not None and rows is not None and sum.untyped_storage().data_ptr() == x.untyped_storage().data_ptr():
-        raise ValueError("sum cannot share memory with x where rows are listed: other rows may still be read")
-    code = _x_code(calls, x)
-    rc = calls.rms(_at(x, x.dtype, device, 0, "x"), code,
-                   0 if add is None else _at(add, calls.bf16, device, 0, "add"),
-                   0 if rows is None else _at(rows, calls.int32, device, n_rows, "rows"), n_rows, hidden,
-                   _at(gain, calls.bf16, device, hidden, "gain"), eps,
-                   0 if sum is None else _at(sum, x.dtype, device, n_rows * hidden, "sum"),
-                   _at(q, calls.e4m3, device, n_rows * hidden, "q"),
-                   _at(scales, calls.e8m0, device, n_rows * fp8_scale_pitch(hidden), "scales"), calls.stream(device))
+    rc = (_fp8_calls or _fp8()).rms(x, add, rows, n_rows, gain, eps, q, scales, sum)
     if rc:
         _check(rc)
 
 
-def _linear_fp8_operands(calls, device, a, a_scales, w, w_scales, bias):
-    if a.dim() != 2 or w.dim() != 2:
-        raise ValueError("a and w must be [rows, k]")
-    (m, k), (n, k_w) = a.shape, w.shape
-    if k_w != k or (bias is not None and bias.numel() != n):
-        raise ValueError("shape mismatch")
-    _fits_int32(m, k)
-    _fits_int32(n, k)
-    pitch = fp8_scale_pitch(k)
-    return m, n, k, (_at(a, calls.e4m3, device, 0, "a"), _at(a_scales, calls.e8m0, device, m * pitch, "a_scales"),
-                     _at(w, calls.e4m3, device, 0, "w"), _at(w_scales, calls.e8m0, device, -(-n // FP8_BLOCK) * pitch, "w_scales"),
-                     0 if bias is None else _at(bias, calls.bf16, device, n, "bias"))
-
-
 def hero_linear_fp8(a, a_scales, w, w_scales, bias, c, act: int = 0, scratch=None):
     """c (bfloat16) = act(a w^T + bias); bias may be None, scratch is an optional contiguous device tensor."""
-    calls, device = _fp8(a)
-    m, n, k, operands = _linear_fp8_operands(calls, device, a, a_scales, w, w_scales, bias)
-    rc = calls.linear(*operands, _at(c, calls.bf16, device, m * n, "c"), m, n, k, act, *_scratch_at(scratch, device),
-                      calls.stream(device))
+    rc = (_fp8_calls or _fp8()).linear(a, a_scales, w, w_scales, bias, c, act, scratch)
     if rc:
         _check(rc)
 
 
 def hero_linear_fp8_quantized(a, a_scales, w, w_scales, bias, q, scales, act: int = 0, scratch=None):
     """hero_linear_fp8 with the result in 8 bits: q, scales are the `a`, `a_scales` of a next product."""
-    calls, device = _fp8(a)
-    m, n, k, operands = _linear_fp8_operands(calls, device, a, a_scales, w, w_scales, bias)
-    rc = calls.linear_quantized(*operands, _at(q, calls.e4m3, device, m * n, "q"),
-                                _at(scales, calls.e8m0, device, m * fp8_scale_pitch(n), "scales"), m, n, k, act,
-                                *_scratch_at(scratch, device), calls.stream(device))
+    rc = (_fp8_calls or _fp8()).linear_quantized(a, a_scales, w, w_scales, bias, q, scales, act, scratch)
     if rc:
         _check(rc)
 

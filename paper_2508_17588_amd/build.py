@@ -1,4 +1,5 @@
-"""Builds libhero.so (the C-ABI library) from the HIP sources for gfx950 with hipcc."""
+"""Builds libhero.so (the C-ABI library) from the HIP sources for gfx950 with hipcc, and _fp8_binding.so, the host module that
+makes the 8-bit calls from Python, with the host compiler."""
 from __future__ import annotations
 
 import os
@@ -10,6 +11,7 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 BUILD_DIR = os.path.join(HERE, "_build")
 LIB_PATH = os.path.join(HERE, "libhero.so")
+BINDING_PATH = os.path.join(HERE, "_fp8_binding.so")
 SOURCES = ["hero_api.hip", "rowops.hip", "gemm.hip", "attention.hip", "narrow.hip", "fp8_rows.hip", "gemm_fp8.hip"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = ["--offload-arch=gfx950", "-O3", "-fPIC", "-std=c++17", "-Wall", "-Wno-unused-function",
@@ -30,16 +32,32 @@ def _compile(src: str, extra=()) -> str:
     return obj
 
 
+def _build_binding() -> None:
+    import sysconfig
+
+    import torch
+    from torch.utils.cpp_extension import include_paths, library_paths
+    cmd = [os.environ.get("CXX", "g++"), "-O2", "-fPIC", "-shared", "-std=c++17", "-Wall",
+           f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}", "-I" + sysconfig.get_paths()["include"],
+           *(a for p in include_paths() for a in ("-isystem", p)), os.path.join(CSRC, "fp8_binding.cpp"), "-o", BINDING_PATH,
+           *("-L" + p for p in library_paths()), "-ltorch_python", "-ltorch_cpu", "-lc10"]
+    res = subprocess.run(cmd, capture_output=True, text=True)
+    if res.returncode != 0:
+        raise RuntimeError("compiling fp8_binding.cpp failed:\n" + res.stdout + res.stderr)
+
+
 def build(verbose: bool = True, extra=()) -> str:
     os.makedirs(BUILD_DIR, exist_ok=True)
-    with ThreadPoolExecutor(max_workers=7) as ex:
+    with ThreadPoolExecutor(max_workers=8) as ex:
+        binding = ex.submit(_build_binding)
         objs = list(ex.map(lambda s: _compile(s, extra), SOURCES))
+        binding.result()
     cmd = [HIPCC, "--offload-arch=gfx950", "-shared", "-fPIC", "-o", LIB_PATH, *objs]
     res = subprocess.run(cmd, capture_output=True, text=True)
     if res.returncode != 0:
         raise RuntimeError("link failed:\n" + res.stdout + res.stderr)
     if verbose:
-        print(f"built {LIB_PATH}")
+        print(f"built {LIB_PATH} and {BINDING_PATH}")
     return LIB_PATH
 
 

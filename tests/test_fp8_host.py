@@ -12,8 +12,8 @@ from paper_2508_17588_amd import binding as B
 @pytest.fixture(scope="module")
 def lib():
     import os
-    if not os.path.exists(B.LIB_PATH):
-        from paper_2508_17588_amd.build import build
+    from paper_2508_17588_amd.build import BINDING_PATH, build
+    if not (os.path.exists(B.LIB_PATH) and os.path.exists(BINDING_PATH)):
         build(verbose=False)
     return B.load_library()
 
@@ -94,14 +94,6 @@ def test_largest_products(lib, m, n, k, what):
     assert lib.hero_linear_fp8(P, P, P, P, P, P, m, n, k, 0, None, 0, None) == B.HERO_ERR_SHAPE and what in lib.hero_last_error()
 
 
-def test_binding_refuses_sizes_past_31_bits():
-    """(A size that the C call's argument cannot hold would otherwise arrive as its low 32 bits.)"""
-    for sizes in ((1 << 31, 16), (1 << 32, 16), (16, 1 << 31)):
-        with pytest.raises(ValueError, match="2\\^31"):
-            B._fits_int32(*sizes)
-    B._fits_int32((1 << 31) - 1, 16)
-
-
 def test_route(lib):
     t = [ctypes.c_int32() for _ in range(3)]
     p = [ctypes.byref(v) for v in t]
@@ -117,7 +109,7 @@ def test_route(lib):
                 assert -(-tiles // 8) * 8 % 256 * last * bm * bn * 4 <= scratch
 
 
-def test_binding_refuses_what_does_not_fit():
+def test_binding_refuses_what_does_not_fit(lib):
     q, s = B.empty_fp8(4, 64, device="cpu")
     x = torch.zeros(4, 64)
     assert s.shape == (4, 4) and B.empty_fp8(300, 64, 128, device="cpu")[1].shape == (3, 4)
@@ -127,3 +119,7 @@ def test_binding_refuses_what_does_not_fit():
         B.hero_linear_fp8(q, s, q, s, None, x)
     with pytest.raises((TypeError, ValueError)):
         B.hero_gather_rms_fp8(x, None, None, 4, torch.zeros(64, dtype=torch.bfloat16), 1e-6, q, s)
+    with pytest.raises(TypeError, match="c must be a tensor|not a device tensor"):
+        B.hero_linear_fp8(q, s, q, s, None, None)
+    with pytest.raises(TypeError, match="x must be a tensor"):
+        B.hero_quantize_fp8([1.0], q, s)

@@ -553,3 +553,70 @@ def test_two_graphs_with_one_scratch():
             torch.cuda.synchronize()
             assert torch.equal(c, want), turn
         scratch.fill_(0xFF)
+
+
+# ---- what the binding refuses before anything is launched ------------------------------------------
+
+def test_binding_refusals():
+    m, n, k = 4, 32, 64
+    a, w, bias = operands(m, n, k)
+    c = torch.zeros(m, n, dtype=torch.bfloat16, device="cuda")
+    q, s = B.empty_fp8(m, n)
+    x, add = torch.randn(m, k, device="cuda"), torch.zeros(m, k, dtype=torch.bfloat16, device="cuda")
+    gain, rows = torch.ones(k, dtype=torch.bfloat16, device="cuda"), torch.zeros(2, dtype=torch.int32, device="cuda")
+    xq, xs = B.empty_fp8(m, k)
+
+    def refused(kind, match, call, *args):
+        with pytest.raises(kind, match=match):
+            call(*args)
+    rms, linear, both, quantize = B.hero_gather_rms_fp8, B.hero_linear_fp8, B.hero_linear_fp8_quantized, B.hero_quantize_fp8
+    # type, order, place and size of each tensor
+    refused(TypeError, "q must be", quantize, x, xs, xs)
+    refused(TypeError, "scales must be", quantize, x, xq, xq)
+    refused(ValueError, "q is too small", quantize, x, xq[:3], xs)
+    refused(ValueError, "scales is too small", quantize, x, xq, xs[:3])
+    refused(ValueError, "rows, columns", quantize, x[0], xq, xs)
+    refused(ValueError, "block_rows", quantize, x, xq, xs, 64)
+    refused(TypeError, "x must be", quantize, x[:, ::2], xq, xs)
+    refused(TypeError, "unsupported", quantize, x.double(), xq, xs)
+    refused(TypeError, "q must be", quantize, x, xq.cpu(), xs)
+    refused(TypeError, "an integer|integer", quantize, x, xq, xs, None)
+    refused(ValueError, "shape", rms, x, add[:3], None, m, gain, 1e-6, xq, xs)
+    refused(ValueError, "shape", rms, x, None, None, m + 1, gain, 1e-6, xq, xs)
+    refused(ValueError, "shape", rms, x, None, None, m, gain[:32], 1e-6, xq, xs)
+    refused(TypeError, "add must be", rms, x, x, None, m, gain, 1e-6, xq, xs)
+    refused(TypeError, "rows must be", rms, x, None, rows.long(), 2, gain, 1e-6, xq, xs)
+    refused(ValueError, "rows is too small", rms, x, None, rows, 3, gain, 1e-6, xq, xs)
+    refused(ValueError, "share memory", rms, x, None, rows, 2, gain, 1e-6, xq, xs, x)
+    refused(TypeError, "sum must be", rms, x, None, None, m, gain, 1e-6, xq, xs, add)
+    refused(TypeError, "real number", rms, x, None, None, m, gain, "1e-6", xq, xs)
+    refused(ValueError, "shape", linear, *a, w[0][:, :32].contiguous(), w[1], bias, c)
+    refused(ValueError, "shape", linear, *a, *w, bias[:16], c)
+    refused(ValueError, "w_scales is too small", linear, *a, w[0], w[1][:0], bias, c)
+    refused(ValueError, "c is too small", linear, *a, *w, bias, c[:3])
+    refused(TypeError, "bias must be", linear, *a, *w, bias.float(), c)
+    refused(TypeError, "scratch must be a tensor", linear, *a, *w, bias, c, 0, 4096)
+    refused(TypeError, "w must be", linear, *a, torch.empty(k, n, dtype=torch.float8_e4m3fn, device="cuda").t(), w[1], None, c)
+    refused(ValueError, "q is too small", both, *a, *w, bias, q[:3], s)
+    refused(ValueError, "scales is too small", both, *a, *w, bias, q, s[:3])
+    refused(TypeError, "a_scales must be a tensor", both, a[0], None, *w, bias, q, s)
+    # the library's own refusals arrive as its error
+    refused(B.HeroError, "act must be", linear, *a, *w, bias, c, 2)
+    refused(B.HeroError, "eps", rms, x, None, None, m, gain, -1.0, xq, xs)
+    refused(B.HeroError, "16-byte", linear, *a, *w, bias, torch.zeros(m * n + 4, dtype=torch.bfloat16, device="cuda")[4:].view(m, n))
+    # sizes past 31 bits do not arrive as their low 32 bits
+    refused(ValueError, "2.31", quantize, torch.zeros(1, 16, device="cuda").expand((1 << 32) + 1, 16), xq, xs)
+    refused(ValueError, "2.31", rms, x, None, rows, (1 << 32) + 1, gain, 1e-6, xq, xs)
+    refused(ValueError, "2.31", linear, a[0][:1].expand((1 << 32) + 1, k), a[1], *w, None, c)
+    torch.cuda.synchronize()
+
+
+def test_calls_on_no_rows():
+    gain = torch.ones(64, dtype=torch.bfloat16, device="cuda")
+    empty, (q, s) = torch.empty(0, 64, device="cuda"), B.empty_fp8(0, 64)
+    B.hero_quantize_fp8(empty, q, s)
+    B.hero_gather_rms_fp8(empty, None, None, 0, gain, 1e-6, q, s, empty.clone())
+    w = operands(1, 32, 64)[1]
+    B.hero_linear_fp8(q, s, *w, None, torch.empty(0, 32, dtype=torch.bfloat16, device="cuda"))
+    B.hero_linear_fp8_quantized(q, s, *w, None, *B.empty_fp8(0, 32))
+    torch.cuda.synchronize()
