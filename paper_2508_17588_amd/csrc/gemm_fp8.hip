@@ -964,6 +964,8 @@ hipError_t launch_quarters(const GemmFp8Args& g, const Grid& grid, hipStream_t s
 // TILE_16 to TILE_64x128: whose waves share k; 8-bit results: 16 x 128, 32 x 128 and 64 x 128
 enum TileKind { TILE_16, TILE_32, TILE_32x64, TILE_64, TILE_64x128, TILE_128, TILE_192x128, TILE_192, TILE_256 };
 
+constexpr int TWO_SLOTS = 16;        // stages of 16 x 16 tiles that eight waves hold in two slots each
+
 template <bool QUANT, bool GELU>
 hipError_t launch_kind(const GemmFp8Args& g, TileKind kind, int chunks, hipStream_t st) {
   const int stages = (g.k + BK - 1) / BK;
@@ -973,7 +975,7 @@ hipError_t launch_kind(const GemmFp8Args& g, TileKind kind, int chunks, hipStrea
       // inputs in turns, 6.6 with four slots), else four (149 x 816 x 3008 8.2 -> 6.8).  A block of 128 columns: four waves with two
       // slots for the fewest stages (8160 columns, two stages: 3.9 us, eight waves with a slot 4.2), else eight (5 x 304 x 7344: 11.1, 12.8)
       if constexpr (QUANT) return stages <= 4 ? launch_shared<1, 8, 4, 2, QUANT, GELU>(g, st) : launch_shared<1, 8, 8, 1, QUANT, GELU>(g, st);
-      else return stages <= 16 ? launch_shared<1, 1, 8, 2, QUANT, GELU>(g, st) : launch_shared<1, 1, 8, 4, QUANT, GELU>(g, st);
+      else return stages <= TWO_SLOTS ? launch_shared<1, 1, 8, 2, QUANT, GELU>(g, st) : launch_shared<1, 1, 8, 4, QUANT, GELU>(g, st);
     case TILE_32:
       if constexpr (QUANT) return launch_shared<2, 8, 6, 1, QUANT, GELU>(g, st);
       else return launch_shared<2, 2, 8, 2, QUANT, GELU>(g, st);
@@ -1038,6 +1040,9 @@ TileChoice choose_tile(const GemmFp8Args& g) {
   for (int kind = TILE_16; kind <= TILE_64x128; ++kind) {
     const SharedCost& c = SHARED_COST[kind][quant];
     if (c.bm == 0 || (stages + c.waves - 1) / c.waves > SHARED_STAGES) continue;
+    // (up to 16 rows: no tile that is half empty, where 16 x 16 has two workgroups to a CU: 1 x 7680 x 1920 5.2 us, in tiles of 32 x 32 5.6;
+    // 5 x 5488 x 1136 3.7, 4.0)
+    if (quant == 0 && kind > TILE_16 && g.m <= 16 && stages <= TWO_SLOTS) continue;
     const int64_t tiles = (int64_t)((g.m + c.bm - 1) / c.bm) * ((g.n + c.bn - 1) / c.bn), a_cu = (tiles + 255) / 256;
     if (tiles > (1 << 20)) continue;
     consider((TileKind)kind, 1, c.fixed + c.stage * ((stages + c.waves - 1) / c.waves) + c.group * a_cu +
@@ -1053,7 +1058,8 @@ TileChoice choose_tile(const GemmFp8Args& g) {
     const double before = rounds_cost(c, whole, stages);
     if (kind == TILE_256)
       consider(TILE_256, -1, before + (whole > 0 ? SECOND_LAUNCH : 0.0) + rounds_cost(TILE_COST[0][quant], 4 * (tiles - whole), stages));
-    for (int s = 2; s <= MOST_CHUNKS && stages / s >= LEAST_STAGES && g.scratch != nullptr; ++s) {
+    if (g.scratch == nullptr || before + c.fixed + FIXUP >= best) continue;
+    for (int s = 2; s <= MOST_CHUNKS && stages / s >= LEAST_STAGES; ++s) {
       const size_t bytes = (size_t)rem * s * c.bm * c.bn * 4;
       if (bytes > g.scratch_bytes) break;
       consider((TileKind)kind, s, before + rounds_cost(c, rem * s, (double)stages / s) + FIXUP + FIXUP_PER_MB * 1e-6 * (double)bytes);

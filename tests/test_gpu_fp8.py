@@ -242,7 +242,7 @@ def test_linear_many_tiles(m, n, k, quantized):
 # Every kernel that a product can go to: the tile and what becomes of the last round's tiles, with 64 MiB of scratch
 SCRATCH = 64 << 20
 ROUTES = [
-    (1, 16, 16, False, (16, 16, 1)), (4, 928, 2064, False, (16, 16, 1)), (9, 7520, 1936, False, (32, 32, 1)),
+    (1, 16, 16, False, (16, 16, 1)), (4, 928, 2064, False, (16, 16, 1)), (9, 7520, 1936, False, (16, 16, 1)),
     (65, 832, 16, False, (32, 32, 1)), (61, 1920, 7696, False, (32, 32, 1)), (161, 1888, 16, False, (32, 64, 1)),
     (550, 720, 3008, False, (32, 64, 1)), (137, 2608, 8160, False, (32, 64, 1)), (12309, 16, 16, False, (64, 64, 1)),
     (400, 1936, 1920, False, (64, 64, 1)), (329, 2192, 3792, False, (64, 64, 1)), (5475, 144, 496, False, (64, 128, 1)),
