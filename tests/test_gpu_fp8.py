@@ -620,3 +620,36 @@ def test_calls_on_no_rows():
     B.hero_linear_fp8(q, s, *w, None, torch.empty(0, 32, dtype=torch.bfloat16, device="cuda"))
     B.hero_linear_fp8_quantized(q, s, *w, None, *B.empty_fp8(0, 32))
     torch.cuda.synchronize()
+
+
+def test_two_threads():
+    """Calls from two threads, each on its own stream with its own results; a refusal in one leaves the other alone."""
+    import threading
+    say("two threads")
+    problems = [operands(226, 400, 1920), operands(40, 528, 4112, seed=20)]
+    wants = [run_linear(a, w, bias, 1, False).clone() for a, w, bias in problems]
+    failures = []
+
+    def work(i):
+        try:
+            a, w, bias = problems[i]
+            side = torch.cuda.Stream()
+            scratch = torch.empty(16 << 20, dtype=torch.uint8, device="cuda")
+            side.wait_stream(torch.cuda.current_stream())
+            with torch.cuda.stream(side):
+                for turn in range(40):
+                    c = torch.zeros_like(wants[i])
+                    B.hero_linear_fp8(*a, *w, bias, c, 1, scratch)
+                    if turn % 8 == i:
+                        with pytest.raises(B.HeroError, match="act must be" if i else "16-byte"):
+                            B.hero_linear_fp8(*a, *w, bias, c if i else torch.empty(c.numel() + 1, dtype=c.dtype, device="cuda")[1:], 2 if i else 0)
+                    side.synchronize()
+                    assert torch.equal(c, wants[i]), turn
+        except BaseException as e:      # (a thread's own failure would pass unseen)
+            failures.append(e)
+    threads = [threading.Thread(target=work, args=(i,)) for i in range(2)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert not failures, failures
