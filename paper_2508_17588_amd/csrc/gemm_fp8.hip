@@ -104,7 +104,7 @@ __device__ __forceinline__ int chunk_begin(int chunk, int n_chunks, const Diviso
 __device__ __forceinline__ uint32_t weight_scale_word(const GemmFp8Args& g, int n, int pitch, int word) {
   typedef const __attribute__((address_space(4))) uint32_t* scalar_t;
   const uint32_t row = (uint32_t)min(n, g.n - 1) / 128u;
-  const uint64_t at = (uint64_t)g.w_scales + (uint64_t)(row * (uint32_t)pitch) + 4u * (uint32_t)min(word, pitch / 4 - 1);
+  const uint64_t at = (uint64_t)g.w_scales + (uint64_t)(row * (uint32_t)pitch) + (uint32_t)fp8_scale_word_offset(word, pitch);
   return *(scalar_t)at;
 }
 
@@ -288,8 +288,9 @@ __global__ __launch_bounds__(512) void gemm256_fp8_kernel(Args256 args) {
     const uint32_t at = (uint32_t)(m0 + wm0 + (l & 31)) * (uint32_t)pitch;
 #pragma unroll
     for (int w = 0; w < WORDS; ++w) {
-      nextA[0][w] = __builtin_amdgcn_raw_buffer_load_b32(rsSA, at, stage + 4 * w, 0);
-      nextA[1][w] = __builtin_amdgcn_raw_buffer_load_b32(rsSA, at + 32u * (uint32_t)pitch, stage + 4 * w, 0);
+      const int word = fp8_scale_word_offset(stage / 4 + w, pitch);
+      nextA[0][w] = __builtin_amdgcn_raw_buffer_load_b32(rsSA, at, word, 0);
+      nextA[1][w] = __builtin_amdgcn_raw_buffer_load_b32(rsSA, at + 32u * (uint32_t)pitch, word, 0);
       nextW[w] = weight_scale_word(g, n0 + wn0, pitch, stage / 4 + w);
     }
   };
@@ -628,7 +629,8 @@ __global__ __launch_bounds__(512) void gemm_fp8_halfk_kernel(GemmFp8Args g, Grid
 #pragma unroll
     for (int w = 0; w < WORDS; ++w) {
 #pragma unroll
-      for (int i = 0; i < MB; ++i) nextA[i][w] = __builtin_amdgcn_raw_buffer_load_b32(rsSA, offSA + 32u * i * (uint32_t)pitch, stage + 4 * w, 0);
+      for (int i = 0; i < MB; ++i)
+        nextA[i][w] = __builtin_amdgcn_raw_buffer_load_b32(rsSA, offSA + 32u * i * (uint32_t)pitch, fp8_scale_word_offset(stage / 4 + w, pitch), 0);
 #pragma unroll
       for (int j = 0; j < NW; ++j) nextW[j][w] = weight_scale_word(g, n0 + wn0 + 32 * j, pitch, stage / 4 + w);
     }

@@ -195,6 +195,10 @@ void attention_route(const AttnArgs& a, int* queries, int* key_ranges);
 
 // 8-bit rows and weights: e4m3 elements, one E8M0 scale a block of 128 (include/hero.h)
 constexpr int fp8_scale_pitch(int columns) { return (columns / 512 + (columns % 512 != 0)) * 4; }
+// Byte offset of scale word `word` within its row; past the row's last word, the last.  Kernels ask for whole groups of words
+// ahead, as far as past the row, and the advance goes into a buffer load's scalar offset, which the bounds check is not taken to
+// cover: without the limit the last row's loads would leave the buffer.
+constexpr int fp8_scale_word_offset(int word, int pitch) { return 4 * (word < pitch / 4 ? word : pitch / 4 - 1); }
 
 struct Fp8Out {
   uint8_t* q = nullptr;            // [rows, columns]
