@@ -377,10 +377,12 @@ int hero_quantize_fp8(const void* dev_x, int32_t x_dtype, int32_t n_rows, int32_
 
 /* h = x[rows[i],:] (+ add[rows[i],:]); out row i = h * gain / sqrt(mean(h^2) + eps) in 8 bits [n_rows, hidden], scales
  * [n_rows, pitch].  rows == NULL means rows[i] = i; rows may repeat.  add may be NULL.  With dev_sum row i of
- * [n_rows, hidden], of x's type, is set to h: the residual's addition.  dev_sum may be dev_x itself where rows is NULL (each
- * row is read before it is written), and overlaps no input otherwise.  The norm uses h before it is rounded for storage.  hidden a multiple
- * of 16, <= 16384.  Statistics in fp32, of the row scaled by a power of two where h^2 or its sum would
- * leave fp32's range: h may be any finite numbers.  A row of zeros with eps 0 is NaN (0 / 0), an infinity a NaN element among zeros. */
+ * [n_rows, hidden], of x's type, is set to h: the residual's addition.  The norm uses h before it is rounded for storage.
+ * dev_sum may be dev_x itself, or dev_add itself where x is bf16 too, if rows is NULL (each row is read before it is written),
+ * and overlaps no input otherwise, else HERO_ERR_INVALID_ARG.  (How many rows x and add have is not known here where some are
+ * listed: only the first is looked at, the rest is the caller's to see to.)
+ * hidden a multiple of 16, <= 16384.  Statistics in fp32, of the row scaled by a power of two where h^2 or its sum would leave
+ * fp32's range: h may be any finite numbers.  A row of zeros with eps 0 is NaN (0 / 0), an infinity a NaN element among zeros. */
 int hero_gather_rms_fp8(const void* dev_x, int32_t x_dtype, const void* dev_add_bf16, const int32_t* dev_rows,
                         int32_t n_rows, int32_t hidden, const void* gain, float eps, void* dev_sum,
                         void* dev_out_q, void* dev_out_scales, void* stream);

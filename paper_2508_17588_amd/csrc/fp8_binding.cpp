@@ -71,6 +71,11 @@ void* address(const at::Tensor* t, at::ScalarType type, const Place& at, int64_t
   return t == nullptr ? nullptr : address(*t, type, at, least, name);
 }
 
+bool overlap(const void* a, int64_t a_bytes, const void* b, int64_t b_bytes) {
+  return a != nullptr && b != nullptr && a_bytes > 0 && b_bytes > 0 && (uintptr_t)a < (uintptr_t)b + (uint64_t)b_bytes &&
+         (uintptr_t)b < (uintptr_t)a + (uint64_t)a_bytes;
+}
+
 int32_t activation(const at::Tensor& x) {
   if (x.scalar_type() == at::kFloat) return HERO_DTYPE_FP32;
   if (x.scalar_type() != at::kBFloat16) refuse(PyExc_TypeError, "unsupported activation dtype %s", c10::toString(x.scalar_type()));
@@ -144,14 +149,16 @@ PyObject* rms(PyObject*, PyObject* const* a, Py_ssize_t n) {
     const int64_t elements = (int64_t)n_rows * hidden;
     if (gain.numel() != hidden || (add && add->numel() != size) || (!rows && size < elements))
       refuse(PyExc_ValueError, "shape mismatch%s");
-    if (sum && rows && sum->storage().data() == x.storage().data())
-      refuse(PyExc_ValueError, "sum cannot share memory with x where rows are listed: other rows may still be read%s");
     const int32_t type = activation(x);
     const void* from = address(x, x.scalar_type(), p, 0, "x");
     const void* branch = address(add, at::kBFloat16, p, 0, "add");
     const int32_t* list = (const int32_t*)address(rows, at::kInt, p, n_rows, "rows");
     const void* gains = address(gain, at::kBFloat16, p, hidden, "gain");
     void* total = address(sum, x.scalar_type(), p, elements, "sum");
+    // (the library does not know how many rows there are to be listed)
+    const int64_t written = elements * x.element_size();
+    if (rows && (overlap(total, written, from, x.nbytes()) || overlap(total, written, branch, add ? add->nbytes() : 0)))
+      refuse(PyExc_ValueError, "sum cannot share memory with x or add where rows are listed: other rows may still be read%s");
     void* to = address(q, at::kFloat8_e4m3fn, p, elements, "q");
     void* to_scales = address(scales, at::kFloat8_e8m0fnu, p, (int64_t)n_rows * HERO_FP8_SCALE_PITCH(hidden), "scales");
     return unlocked([&] { return calls.rms(from, type, branch, list, n_rows, hidden, gains, (float)eps, total, to, to_scales, p.stream); });

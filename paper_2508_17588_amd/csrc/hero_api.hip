@@ -43,6 +43,11 @@ bool aligned16(std::initializer_list<const void*> ptrs) {
   return true;
 }
 
+// Do two ranges share a byte?  (a null one holds none)
+bool overlap(const void* a, int64_t a_bytes, const void* b, int64_t b_bytes) {
+  return a && b && a_bytes > 0 && b_bytes > 0 && (uintptr_t)a < (uintptr_t)b + (uint64_t)b_bytes && (uintptr_t)b < (uintptr_t)a + (uint64_t)a_bytes;
+}
+
 // 8-bit operands are addressed with 32-bit byte offsets, and so are 256 rows of a result; a launch has less than 2^32 threads
 const char* fp8_misfit(int64_t m, int64_t n, int64_t k) {
   if ((m + 512) * k >= (int64_t)1 << 32 || (n + 512) * k >= (int64_t)1 << 32)
@@ -1116,12 +1121,16 @@ int hero_gather_rms_fp8(const void* dev_x, int32_t x_dtype, const void* dev_add_
   if (hidden < 16 || hidden % 16 != 0 || hidden > 16384) return fail(HERO_ERR_SHAPE, "hidden must be a multiple of 16, <= 16384");
   if (!aligned16({dev_x, dev_add_bf16, gain, dev_sum, dev_out_q}) || ((uintptr_t)dev_rows & 3) || ((uintptr_t)dev_out_scales & 3))
     return fail(HERO_ERR_INVALID_ARG, "x, add, gain, sum and out_q must be 16-byte aligned, rows and out_scales 4-byte aligned");
-  if (dev_sum && dev_rows && dev_sum == dev_x)
-    return fail(HERO_ERR_INVALID_ARG, "sum cannot be x itself where rows are listed: other rows may still be read");
-  if (dev_sum && !dev_rows && dev_sum != dev_x) {
-    const uintptr_t bytes = (uintptr_t)n_rows * hidden * (x_dtype == HERO_DTYPE_FP32 ? 4 : 2), d = (uintptr_t)dev_sum - (uintptr_t)dev_x;
-    if (d < bytes || 0 - d < bytes) return fail(HERO_ERR_INVALID_ARG, "sum may be x itself, but not overlap it otherwise");
-  }
+  // (of listed rows nobody here knows how many the inputs have: one at least)
+  const int64_t x_size = x_dtype == HERO_DTYPE_FP32 ? 4 : 2, written = (int64_t)n_rows * hidden, read = dev_rows ? std::min(n_rows, 1) * (int64_t)hidden : written;
+  if (dev_rows && overlap(dev_sum, written * x_size, dev_x, read * x_size))
+    return fail(HERO_ERR_INVALID_ARG, "sum cannot overlap x where rows are listed: other rows may still be read");
+  if (dev_sum != dev_x && overlap(dev_sum, written * x_size, dev_x, read * x_size))
+    return fail(HERO_ERR_INVALID_ARG, "sum may be x itself, but not overlap it otherwise");
+  const bool is_add = dev_sum == dev_add_bf16 && !dev_rows && x_dtype == HERO_DTYPE_BF16;
+  if ((!is_add && overlap(dev_sum, written * x_size, dev_add_bf16, read * 2)) || overlap(dev_sum, written * x_size, dev_rows, 4 * (int64_t)n_rows) ||
+      overlap(dev_sum, written * x_size, gain, 2 * (int64_t)hidden))
+    return fail(HERO_ERR_INVALID_ARG, "sum cannot overlap add, rows or gain");
   RmsFp8Args a;
   a.x = dev_x; a.x_fp32 = x_dtype == HERO_DTYPE_FP32; a.add = (const bf16_t*)dev_add_bf16; a.rows = dev_rows;
   a.n_rows = n_rows; a.hidden = hidden; a.gain = (const bf16_t*)gain; a.eps = eps; a.sum = dev_sum;
