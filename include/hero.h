@@ -366,7 +366,9 @@ int hero_stability_scores(const double* variances, int32_t n_layers, double* sco
  * last word are written as 127 and never used.  Column counts are multiples of 16.
  * A block is put into 8 bits with the least scale that takes its largest finite magnitude to 448 or below (byte 127 if that is
  * 0; never below byte 0), every element rounded to nearest, ties to even; NaN and infinities become NaN elements and do not
- * count for the scale. */
+ * count for the scale.
+ * What these calls write (scratch too) overlaps neither what they read nor what else they write, else HERO_ERR_INVALID_ARG; one
+ * exception is named below. */
 #define HERO_FP8_BLOCK 128
 #define HERO_FP8_SCALE_PITCH(columns) (((columns) / 512 + ((columns) % 512 != 0)) * 4)
 

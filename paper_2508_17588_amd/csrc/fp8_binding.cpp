@@ -155,12 +155,15 @@ PyObject* rms(PyObject*, PyObject* const* a, Py_ssize_t n) {
     const int32_t* list = (const int32_t*)address(rows, at::kInt, p, n_rows, "rows");
     const void* gains = address(gain, at::kBFloat16, p, hidden, "gain");
     void* total = address(sum, x.scalar_type(), p, elements, "sum");
-    // (the library does not know how many rows there are to be listed)
-    const int64_t written = elements * x.element_size();
-    if (rows && (overlap(total, written, from, x.nbytes()) || overlap(total, written, branch, add ? add->nbytes() : 0)))
-      refuse(PyExc_ValueError, "sum cannot share memory with x or add where rows are listed: other rows may still be read%s");
     void* to = address(q, at::kFloat8_e4m3fn, p, elements, "q");
-    void* to_scales = address(scales, at::kFloat8_e8m0fnu, p, (int64_t)n_rows * HERO_FP8_SCALE_PITCH(hidden), "scales");
+    const int64_t scale_bytes = (int64_t)n_rows * HERO_FP8_SCALE_PITCH(hidden);
+    void* to_scales = address(scales, at::kFloat8_e8m0fnu, p, scale_bytes, "scales");
+    // (the library does not know how many rows there are to be listed)
+    auto reads = [&](const void* out, int64_t bytes) {
+      return overlap(out, bytes, from, x.nbytes()) || overlap(out, bytes, branch, add ? add->nbytes() : 0);
+    };
+    if (rows && (reads(total, elements * x.element_size()) || reads(to, elements) || reads(to_scales, scale_bytes)))
+      refuse(PyExc_ValueError, "sum, q and scales cannot share memory with x or add where rows are listed: other rows may still be read%s");
     return unlocked([&] { return calls.rms(from, type, branch, list, n_rows, hidden, gains, (float)eps, total, to, to_scales, p.stream); });
   });
 }

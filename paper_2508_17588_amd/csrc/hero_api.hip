@@ -48,6 +48,22 @@ bool overlap(const void* a, int64_t a_bytes, const void* b, int64_t b_bytes) {
   return a && b && a_bytes > 0 && b_bytes > 0 && (uintptr_t)a < (uintptr_t)b + (uint64_t)b_bytes && (uintptr_t)b < (uintptr_t)a + (uint64_t)a_bytes;
 }
 
+struct Range {
+  const void* p;
+  int64_t bytes;
+  const char* name;
+};
+// what a call writes overlaps neither what it reads nor what else it writes
+int check_apart(std::initializer_list<Range> written, std::initializer_list<Range> read) {
+  for (const Range* w = written.begin(); w != written.end(); ++w) {
+    for (const Range& r : read)
+      if (overlap(w->p, w->bytes, r.p, r.bytes)) return fail(HERO_ERR_INVALID_ARG, "%s cannot overlap %s", w->name, r.name);
+    for (const Range* o = w + 1; o != written.end(); ++o)
+      if (overlap(w->p, w->bytes, o->p, o->bytes)) return fail(HERO_ERR_INVALID_ARG, "%s cannot overlap %s", w->name, o->name);
+  }
+  return HERO_OK;
+}
+
 // 8-bit operands are addressed with 32-bit byte offsets, and so are 256 rows of a result; a launch has less than 2^32 threads
 const char* fp8_misfit(int64_t m, int64_t n, int64_t k) {
   if ((m + 512) * k >= (int64_t)1 << 32 || (n + 512) * k >= (int64_t)1 << 32)
@@ -1106,6 +1122,10 @@ int hero_quantize_fp8(const void* dev_x, int32_t x_dtype, int32_t n_rows, int32_
   if (!fp8_rows_fit(n_rows, columns)) return fail(HERO_ERR_SHAPE, "n_rows * ceil(columns / 512) must stay below 2^31");
   if (!aligned16({dev_x, dev_out_q}) || ((uintptr_t)dev_out_scales & 3))
     return fail(HERO_ERR_INVALID_ARG, "x and out_q must be 16-byte aligned, out_scales 4-byte aligned");
+  const int64_t elements = (int64_t)n_rows * columns, scale_rows = block_rows == 1 ? n_rows : ((int64_t)n_rows + 127) / 128;
+  if (const int rc = check_apart({{dev_out_q, elements, "out_q"}, {dev_out_scales, scale_rows * HERO_FP8_SCALE_PITCH((int64_t)columns), "out_scales"}},
+                                 {{dev_x, elements * (x_dtype == HERO_DTYPE_FP32 ? 4 : 2), "x"}}))
+    return rc;
   HIP_TRY(launch_quantize_fp8(dev_x, x_dtype == HERO_DTYPE_FP32, n_rows, columns, block_rows,
                               {(uint8_t*)dev_out_q, (uint8_t*)dev_out_scales}, (hipStream_t)stream));
   return HERO_OK;
@@ -1131,6 +1151,10 @@ int hero_gather_rms_fp8(const void* dev_x, int32_t x_dtype, const void* dev_add_
   if ((!is_add && overlap(dev_sum, written * x_size, dev_add_bf16, read * 2)) || overlap(dev_sum, written * x_size, dev_rows, 4 * (int64_t)n_rows) ||
       overlap(dev_sum, written * x_size, gain, 2 * (int64_t)hidden))
     return fail(HERO_ERR_INVALID_ARG, "sum cannot overlap add, rows or gain");
+  if (const int rc = check_apart({{dev_out_q, written, "out_q"}, {dev_out_scales, (int64_t)n_rows * HERO_FP8_SCALE_PITCH(hidden), "out_scales"}},
+                                 {{dev_x, read * x_size, "x"}, {dev_add_bf16, read * 2, "add"}, {dev_rows, 4 * (int64_t)n_rows, "rows"},
+                                  {gain, 2 * (int64_t)hidden, "gain"}, {dev_sum, written * x_size, "sum"}}))
+    return rc;
   RmsFp8Args a;
   a.x = dev_x; a.x_fp32 = x_dtype == HERO_DTYPE_FP32; a.add = (const bf16_t*)dev_add_bf16; a.rows = dev_rows;
   a.n_rows = n_rows; a.hidden = hidden; a.gain = (const bf16_t*)gain; a.eps = eps; a.sum = dev_sum;
@@ -1148,6 +1172,13 @@ static int linear_fp8(GemmFp8Args& g, int32_t act, size_t scratch_bytes, hipStre
   if (const char* why = fp8_misfit(g.m, g.n, g.k)) return fail(HERO_ERR_SHAPE, "%s", why);
   if (!aligned16({g.a, g.w, g.bias, g.c, g.out.q, g.scratch}) || (((uintptr_t)g.a_scales | (uintptr_t)g.w_scales | (uintptr_t)g.out.scales) & 3))
     return fail(HERO_ERR_INVALID_ARG, "a, w, bias, the result and scratch must be 16-byte aligned, scales 4-byte aligned");
+  const int64_t elements = (int64_t)g.m * g.n, pitch = HERO_FP8_SCALE_PITCH((int64_t)g.k);
+  const int64_t scratch_size = (int64_t)std::min(scratch_bytes, (size_t)INT64_MAX);
+  if (const int rc = check_apart({{g.c, 2 * elements, "c"}, {g.out.q, elements, "out_q"},
+                                  {g.out.scales, g.m * (int64_t)HERO_FP8_SCALE_PITCH((int64_t)g.n), "out_scales"}, {g.scratch, scratch_size, "scratch"}},
+                                 {{g.a, (int64_t)g.m * g.k, "a"}, {g.a_scales, g.m * pitch, "a_scales"}, {g.w, (int64_t)g.n * g.k, "w"},
+                                  {g.w_scales, ((int64_t)g.n + 127) / 128 * pitch, "w_scales"}, {g.bias, 2 * (int64_t)g.n, "bias"}}))
+    return rc;
   g.gelu = act != 0;
   g.scratch_bytes = g.scratch ? scratch_bytes : 0;
   HIP_TRY(launch_gemm_fp8(g, st));

@@ -109,3 +109,84 @@ def test_binding_looks_at_all_rows_of_x_and_add(dtype):
     # nothing listed: two tensors without memory do not overlap
     none = torch.empty(0, hidden, dtype=dtype, device="cuda")
     B.hero_gather_rms_fp8(none, None, rows[:0], 0, gain, 1e-6, *B.empty_fp8(0, hidden), none.clone())
+
+
+# ---- every other output, and scratch ----------------------------------------------------------------------------------------
+
+def overlaps(sizes, written, call):
+    """`call(places)` with one buffer of `written` moved onto another: the last bytes of one on the first of the other."""
+    base = {name: AT + (i << 20) for i, name in enumerate(sizes)}
+    for w in written:
+        for other in sizes:
+            if other == w:
+                continue
+            places = dict(base, **{w: base[other] - sizes[w] + 16 if sizes[w] % 16 == 0 else base[other]})
+            if places[w] % 16:
+                places[w] = base[other]
+            yield w, other, call(places)
+            yield w, other, call(dict(base, **{w: base[other] + (sizes[other] - 1) // 16 * 16}))
+
+
+def refused(lib, sizes, written, call):
+    for w, other, rc in overlaps(sizes, written, call):
+        assert rc == B.HERO_ERR_INVALID_ARG and b"overlap" in lib.hero_last_error(), (w, other)
+
+
+@pytest.mark.parametrize("dtype", [0, 1])
+@pytest.mark.parametrize("block_rows", [1, 128])
+def test_quantize_outputs(lib, dtype, block_rows):
+    n, cols = 256, 640
+    sizes = {"x": n * cols * (4 if dtype else 2), "q": n * cols, "scales": n // block_rows * 8}
+    refused(lib, sizes, ("q", "scales"), lambda p: lib.hero_quantize_fp8(at(p["x"]), dtype, n, cols, block_rows, at(p["q"]), at(p["scales"]), None))
+
+
+@pytest.mark.parametrize("listed", [False, True])
+def test_norm_outputs(lib, listed):
+    n, hidden = 16, 640
+    reads = 1 if listed else n
+    sizes = {"x": reads * hidden * 4, "add": reads * hidden * 2, "gain": hidden * 2, "sum": n * hidden * 4, "q": n * hidden, "scales": n * 8}
+    if listed:
+        sizes["rows"] = 4 * n
+    refused(lib, sizes, ("q", "scales"),
+            lambda p: lib.hero_gather_rms_fp8(at(p["x"]), 1, at(p["add"]), at(p.get("rows")), n, hidden, at(p["gain"]), 1e-6, at(p["sum"]),
+                                              at(p["q"]), at(p["scales"]), None))
+
+
+@pytest.mark.parametrize("bias", [False, True])
+def test_product_outputs(lib, bias):
+    m, n, k, scratch = 32, 272, 640, 4096
+    sizes = {"a": m * k, "a_scales": m * 8, "w": n * k, "w_scales": 3 * 8, "scratch": scratch}
+    if bias:
+        sizes["bias"] = 2 * n
+    first = lambda p: (at(p["a"]), at(p["a_scales"]), at(p["w"]), at(p["w_scales"]), at(p.get("bias")))
+    refused(lib, dict(sizes, c=2 * m * n), ("c", "scratch"),
+            lambda p: lib.hero_linear_fp8(*first(p), at(p["c"]), m, n, k, 0, at(p["scratch"]), scratch, None))
+    refused(lib, dict(sizes, q=m * n, scales=m * 4), ("q", "scales", "scratch"),
+            lambda p: lib.hero_linear_fp8_quantized(*first(p), at(p["q"]), at(p["scales"]), m, n, k, 0, at(p["scratch"]), scratch, None))
+
+
+@pytest.mark.skipif(torch.cuda.is_available(), reason="the buffers are made up")
+def test_buffers_side_by_side_are_accepted(lib):
+    m, n, k = 32, 256, 512
+    sizes = (("a", m * k), ("a_scales", m * 4), ("w", n * k), ("w_scales", 2 * 4 + 8), ("bias", 2 * n), ("q", m * n), ("scales", m * 4), ("scratch", 4096))
+    p, end = {}, AT
+    for name, size in sizes:
+        p[name], end = at(end), end + size
+    args = (p["a"], p["a_scales"], p["w"], p["w_scales"], p["bias"])
+    without_a_gpu((lib.hero_linear_fp8_quantized(*args, p["q"], p["scales"], m, n, k, 0, p["scratch"], 4096, None), lib.hero_last_error()))
+    without_a_gpu((lib.hero_quantize_fp8(at(AT), 0, m, k, 1, at(AT + 2 * m * k), at(AT + 3 * m * k), None), lib.hero_last_error()))
+
+
+@pytest.mark.gpu
+def test_binding_looks_at_all_rows_for_q_and_scales_too():
+    n, total, hidden = 2, 40, 64
+    x = torch.randn(total, hidden, device="cuda")
+    gain, rows = torch.ones(hidden, dtype=torch.bfloat16, device="cuda"), torch.tensor([3, 1], dtype=torch.int32, device="cuda")
+    q, s = B.empty_fp8(n, hidden)
+    inside = x.view(torch.uint8)[30].view(torch.float8_e4m3fn)[:n * hidden].view(n, hidden)
+    with pytest.raises(ValueError, match="share memory"):
+        B.hero_gather_rms_fp8(x, None, rows, n, gain, 1e-6, inside, s)
+    with pytest.raises(ValueError, match="share memory"):
+        B.hero_gather_rms_fp8(x, None, rows, n, gain, 1e-6, q, inside.view(torch.float8_e8m0fnu))
+    with pytest.raises(B.HeroError, match="overlap"):
+        B.hero_quantize_fp8(x[30:31], inside[:1], s)
