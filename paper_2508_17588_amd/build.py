@@ -51,11 +51,11 @@ def build(verbose: bool = True, extra=()) -> str:
     with ThreadPoolExecutor(max_workers=8) as ex:
         binding = ex.submit(_build_binding)
         objs = list(ex.map(lambda s: _compile(s, extra), SOURCES))
-        binding.result()
     cmd = [HIPCC, "--offload-arch=gfx950", "-shared", "-fPIC", "-o", LIB_PATH, *objs]
     res = subprocess.run(cmd, capture_output=True, text=True)
     if res.returncode != 0:
         raise RuntimeError("link failed:\n" + res.stdout + res.stderr)
+    binding.result()                # (only now: the library needs neither torch's headers nor Python's)
     if verbose:
         print(f"built {LIB_PATH} and {BINDING_PATH}")
     return LIB_PATH
