@@ -373,7 +373,8 @@ int hero_stability_scores(const double* variances, int32_t n_layers, double* sco
 #define HERO_FP8_SCALE_PITCH(columns) (((columns) / 512 + ((columns) % 512 != 0)) * 4)
 
 /* x [n_rows, columns] (fp32 or bf16) in 8 bits: out_q [n_rows, columns], out_scales [ceil(n_rows / block_rows), pitch].
- * block_rows: 1 (activations) or 128 (weights).  The buffers of an empty problem may be NULL. */
+ * block_rows: 1 (activations) or 128 (weights).  The buffers of an empty problem may be NULL.  n_rows * ceil(columns / 512) must stay
+ * below 2^31, columns in blocks of 128 rows at 2^31 - 128 or below, else HERO_ERR_SHAPE. */
 int hero_quantize_fp8(const void* dev_x, int32_t x_dtype, int32_t n_rows, int32_t columns, int32_t block_rows,
                       void* dev_out_q, void* dev_out_scales, void* stream);
 

@@ -1119,6 +1119,7 @@ int hero_quantize_fp8(const void* dev_x, int32_t x_dtype, int32_t n_rows, int32_
   if (x_dtype != HERO_DTYPE_FP32 && x_dtype != HERO_DTYPE_BF16) return fail(HERO_ERR_INVALID_ARG, "bad x_dtype");
   if (block_rows != 1 && block_rows != HERO_FP8_BLOCK) return fail(HERO_ERR_INVALID_ARG, "block_rows must be 1 or 128");
   if (columns < 16 || columns % 16 != 0) return fail(HERO_ERR_SHAPE, "columns must be a multiple of 16");
+  if (block_rows != 1 && columns > INT32_MAX - 127) return fail(HERO_ERR_SHAPE, "columns of 128 x 128 blocks must not pass 2^31 - 128");   // (2^32 threads)
   if (!fp8_rows_fit(n_rows, columns)) return fail(HERO_ERR_SHAPE, "n_rows * ceil(columns / 512) must stay below 2^31");
   if (!aligned16({dev_x, dev_out_q}) || ((uintptr_t)dev_out_scales & 3))
     return fail(HERO_ERR_INVALID_ARG, "x and out_q must be 16-byte aligned, out_scales 4-byte aligned");
