@@ -22,14 +22,14 @@ namespace {
 // 16-byte chunks are XOR-swizzled with (row/2)%8.  A barrier each half stage.  In bytes a stage is that of a bf16 kernel with
 // k steps of 64, and takes the matrix pipe as long (16 MFMAs of 64 cycles a wave), at twice the flops.
 // Bound by the matrix pipes at the clock that the chip's power allows: 8192^3 runs at 2.73 PFLOP/s on random data and at 3.9
-// on zeros (a loop of these MFMAs on registers: 3.2 to 3.8 and 4.6).  17776 x 7680 x 1920 takes 225 to 235 us (2.2 to 2.3
-// PFLOP/s; with GELU into 8 bits 251 to 265, whose epilogues the pipes wait for), 17776 x 1920 x 7680 230.
+// on zeros (a loop of these MFMAs on registers: 3.2 to 3.8 and 4.6).  17776 x 7680 x 1920 takes 225 to 258 us on
+// different cards (2.0 to 2.3 PFLOP/s; with GELU into 8 bits 254 to 286, whose epilogues the pipes wait for), 17776 x 1920 x 7680 222 to 249.
 //  * A wave's 128 columns are one scale block of the weight and, in 8-bit results, one block of the output row: its scale is
 //    found without leaving the wave.
 //  * The last four MFMAs of a half stage run after the next barrier, while the first fragments behind it arrive; a fragment is
 //    read four MFMAs ahead of its use, so four W fragments and two pairs of A fragments are all that is held (64 registers
 //    beside 128 accumulators).
-//  * Workgroups walk over the tiles: the next tile's first fills go out before a result is stored.  (17776 x 7680 x 1920: 264 us
+//  * Workgroups walk over the tiles: the next tile's first fills go out before a result is stored.  (17776 x 7680 x 1920 on one card: 264 us
 //    with W filled a whole stage ahead, 249 in halves, 241 with sums that begin with the bias and tile places found without
 //    divisions, the rest from the last round's quarters.)
 //  * Scale bytes of GROUP stages lie in registers, shifted down a byte a stage; those of the next group are asked for at the
@@ -801,7 +801,7 @@ __global__ __launch_bounds__(256) void gemm_fp8_fixup_kernel(GemmFp8Args g, Grid
 // barrier until the sums meet in LDS.  v_mfma_scale_f32_16x16x128_f8f6f4 (A fragment: lane holds row lane%16 and a quarter of
 // 128 k; accumulator register i of a lane is row 4*(lane/16) + i, column lane%16): a stage of 128 k is one step.
 // Bound by what a CU takes in, 80 to 90 KB/us, after a start of 2 to 3 us: 226 x 1920 x 1920 in tiles of 32 x 64 takes 5.4 us (tiles
-// of 128 x 128 11.8, of 32 x 16 10.2), 128 x 4096 x 4096 8.2 (17.3 cut along k, 16.7), 226 x 1920 x 7680 12.2 (17.2, 22.2);
+// of 128 x 128 11.8, of 32 x 16 10.2), 128 x 4096 x 4096 8.2 (17.3 cut along k, 16.7), 226 x 1920 x 7680 11.7 (17.2, 22.2);
 // 1 x 7680 x 1920 in tiles of 16 x 16 3.7 us back to back, 4 TB/s of weights.  A slot each for eight waves is as good as three
 // each for four.  Operands loaded straight into registers took twice as long: such a load touches 16 lines where one into LDS
 // touches eight.
@@ -1004,7 +1004,9 @@ struct TileChoice { TileKind kind; int chunks; };
 // Expected times (us), fitted to timings of every kind, cut and not, in both result types, those near the fastest weighing
 // most: the tiles from 128 x 128 on to 1900 at 48 sizes (1 .. 17776 rows, n 96 .. 7680, k 64 .. 8192), those whose waves share k to
 // 1000 at 72 (1 .. 2553 rows, n 16 .. 8160, k 192 .. 7872).  At the latter the kind chosen takes 2.4 % longer than the best of all
-// kinds on average, 26 % at most (2 x 416 x 7168 in 8 bits: seven chunks where 16 x 128 tiles are better).
+// kinds on average, 26 % at most (2 x 416 x 7168 in 8 bits: seven chunks where 16 x 128 tiles are better).  At 80 other sizes, drawn
+// afterwards, with 64 MiB of scratch: 1.2 and 27 % at 30 of 1 .. 600 rows, 0.1 and 1.3 % at 30 of 600 .. 17776 rows (all of these
+// with n and k to 8192), 3.7 and 14 % at 20 with k from 8192 to 16384, past what was fitted (1 x 8864 x 11024: 29.0 us, 25.4).
 //
 // Tiles: a round of at most 256 of them, one a CU, takes fixed + stages * rate; the rate rises from `low` to `high` as the last
 // CUs come to work and the chip lowers its clock.  Per round at k = 1920: 128 x 128 14.5, 192 x 128 17.4, 192 x 192 22.4,
@@ -1043,7 +1045,8 @@ TileChoice choose_tile(const GemmFp8Args& g) {
     const SharedCost& c = SHARED_COST[kind][quant];
     if (c.bm == 0 || (stages + c.waves - 1) / c.waves > SHARED_STAGES) continue;
     // (up to 16 rows: no tile that is half empty, where 16 x 16 has two workgroups to a CU: 1 x 7680 x 1920 5.2 us, in tiles of 32 x 32 5.6;
-    // 5 x 5488 x 1136 3.7, 4.0)
+    // 5 x 5488 x 1136 3.7, 4.0.  From 17 stages on the prices are right: 1 x 8192 x 8192 13.7 us in 16 x 16, 12.2 in 32 x 32, 12.7 in
+    // 32 x 64; 1 x 7680 x 2304 7.2, 6.3, 6.4; 16 x 14336 x 4096 15.4, 13.0, 11.9; 1 x 1920 x 7680 5.8, 7.4, 9.9)
     if (quant == 0 && kind > TILE_16 && g.m <= 16 && stages <= TWO_SLOTS) continue;
     const int64_t tiles = (int64_t)((g.m + c.bm - 1) / c.bm) * ((g.n + c.bn - 1) / c.bn), a_cu = (tiles + 255) / 256;
     if (tiles > (1 << 20)) continue;
