@@ -379,7 +379,8 @@ int hero_quantize_fp8(const void* dev_x, int32_t x_dtype, int32_t n_rows, int32_
                       void* dev_out_q, void* dev_out_scales, void* stream);
 
 /* h = x[rows[i],:] (+ add[rows[i],:]); out row i = h * gain / sqrt(mean(h^2) + eps) in 8 bits [n_rows, hidden], scales
- * [n_rows, pitch].  rows == NULL means rows[i] = i; rows may repeat.  add may be NULL.  With dev_sum row i of
+ * [n_rows, pitch].  rows == NULL means rows[i] = i; rows may repeat, and each has to be a row of x (not looked at: they lie on the
+ * device).  add may be NULL.  With dev_sum row i of
  * [n_rows, hidden], of x's type, is set to h: the residual's addition.  The norm uses h before it is rounded for storage.
  * dev_sum may be dev_x itself, or dev_add itself where x is bf16 too, if rows is NULL (each row is read before it is written),
  * and overlaps no input otherwise, else HERO_ERR_INVALID_ARG.  (How many rows x and add have is not known here where some are
